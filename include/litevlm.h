@@ -17,6 +17,12 @@
  *                             litevlm_gather_hidden compacts the hidden states for the LLM)
  * and, for the token generated after the prefill:
  *   litevlm_decode_attn       extend-one decode attention over the compacted KV cache
+ * and, for a generation that keeps its keys and values in 4 bits:
+ *   litevlm_cache4_append     rows of K and V into the 4-bit cache (litevlm_cache4_read: back)
+ *   litevlm_cache4_attn       attention of each sample's newest tokens over its cached rows,
+ *                             with the attention weight that each row receives
+ *   litevlm_cache4_evict      the rows of largest accumulated weight into a smaller cache
+ *   litevlm_verify_draft      drafted tokens against the target's probabilities
  *
  * Conventions shared by every call
  *   - Pointers marked "dev" are device pointers owned by the caller; the library
@@ -480,6 +486,203 @@ litevlm_status_t litevlm_decode_attn(int32_t in_dtype, int32_t out_dtype, int32_
                                      float softmax_scale, float q_scale, float k_scale,
                                      float v_scale, void* o, void* workspace,
                                      size_t workspace_bytes, void* stream);
+
+/*
+ * The 4-bit cache - one device buffer of litevlm_cache4_bytes() bytes that holds,
+ * for each sample b and KV head g (b * Hkv + g, in order), four arrays over the
+ * positions 0..cap-1:
+ *   K codes  uint8 [cap, D/2]     V codes  uint8 [cap, D/2]
+ *   K scales uint8 [D/32, cap]    V scales uint8 [D/32, cap]
+ * A row's elements 2c and 2c+1 are the low and the high four bits of its byte c:
+ * OCP E2M1 codes (sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6). The scale byte e of a
+ * block of 32 elements is OCP E8M0: the block's values are 2^(e-127) times its
+ * codes, and 255 makes them NaN. At D = 128 a token's key or value takes 68 bytes
+ * a head, where bf16 takes 256.
+ *
+ * A block x is stored with the least E in [-125, 125] for which
+ * max|x| <= 7 * 2^E, and codes x * 2^-E rounded to the nearest E2M1 value (ties to
+ * the even code, values beyond 6 to 6): no element is further than 2^E from its
+ * stored value (blocks beyond 7 * 2^125 aside, which saturate). A block
+ * that holds a NaN or an infinity is stored as NaN.
+ *
+ *   cap                positions: a multiple of 32, at most LITEVLM_MAX_CACHE4
+ *   D                  head dim 64 or 128
+ * A position's row is the caller's to keep track of (`lengths`, `start`): the
+ * calls neither read nor write positions that they are not told of, except that
+ * the attention may read, and ignores, rows behind a sample's length.
+ */
+#define LITEVLM_MAX_CACHE4 16777216
+
+/* Bytes of a 4-bit cache: B * Hkv * cap * (D + D/16), 0 when the sizes are invalid. */
+size_t litevlm_cache4_bytes(int32_t B, int32_t Hkv, int32_t D, int32_t cap);
+
+/*
+ * litevlm_cache4_append - quantises rows of keys and values into the 4-bit cache.
+ *
+ * Paper: Experiments section, Deployment paragraph (post-training quantisation
+ * for deployment); Results section (decoding is bound by the pass over the cache).
+ *
+ * Row i of sample b (packed row cu_new[b] + i) goes to position start[b] + i, for
+ * i < min(cu_new[b+1] - cu_new[b], max_new); rows whose position is outside
+ * [0, cap) are not written.
+ *
+ *   dtype              LITEVLM_F32 or LITEVLM_BF16 (k, v)
+ *   B, Hkv, D, cap     batch, KV heads (1..LITEVLM_MAX_HEADS), the cache's sizes
+ *   max_new            host upper bound on the new rows of a sample (0..cap)
+ *   k, v               dev [total, Hkv, D], total = cu_new[B]
+ *   cu_new             dev int32 [B+1], non-decreasing, cu_new[0] = 0
+ *   start              dev int32 [B]: the position of each sample's first new row
+ *   cache              dev, the 4-bit cache (in place)
+ *   weight             dev fp32 [B, Hkv, cap] or NULL: set to 0 at the new positions
+ *                      (the accumulated attention weights of litevlm_cache4_attn)
+ */
+litevlm_status_t litevlm_cache4_append(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap,
+                                       int32_t max_new, const void* k, const void* v, const int32_t* cu_new,
+                                       const int32_t* start, void* cache, float* weight, void* stream);
+
+/*
+ * litevlm_cache4_read - the values of cached rows: packed row cu_rows[b] + i of k
+ * and v is the row at position start[b] + i of sample b, for
+ * i < min(cu_rows[b+1] - cu_rows[b], max_rows); a position outside [0, cap) gives
+ * zeros. Every finite cached value is exact in bf16 and fp32. Arguments as for
+ * litevlm_cache4_append, with k and v the outputs (dtype F32 or BF16).
+ */
+litevlm_status_t litevlm_cache4_read(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap,
+                                     int32_t max_rows, const void* cache, const int32_t* start,
+                                     const int32_t* cu_rows, void* k, void* v, void* stream);
+
+/* Bytes of device workspace litevlm_cache4_attn needs for these sizes (0 when the
+ * sizes are invalid). */
+size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+                                     int32_t max_q, int32_t max_len, int32_t weight_rows);
+
+/*
+ * litevlm_cache4_attn - attention of each sample's newest tokens over its rows of
+ * the 4-bit cache, and the attention weight that each cached row receives.
+ *
+ * Paper: Results section (each output token is decoded against the cached keys
+ * and values); Related Work (candidates verified in one pass with the KV cache;
+ * FastV's attention weight as a token's importance).
+ *
+ * Sample b has n_b = lengths[b] cached rows, its newest tokens' own rows (appended
+ * before) last, and m_b = cu_q[b+1] - cu_q[b] queries; query i sees the rows
+ * j <= n_b - m_b + i:
+ *   p_i,h(j) = softmax_j(q_i,h . K_j,h/G * softmax_scale),   o_i,h = sum_j p_i,h(j) V_j,h/G
+ *   weight_out[b,g,j] = weight_in[b,g,j] + sum_{i < min(weight_rows, m_b)} sum_{h in g} p_i,h(j)
+ * A query that sees no row (m_b > n_b) gives o = 0 and adds no weight. Softmax and
+ * accumulation in fp32. For bf16 queries the probabilities are rounded to bf16
+ * in front of the product with V (the weights and the softmax sum are not); for
+ * fp32 queries every product is exact in fp32. A probability below 2^-126 of its
+ * row's largest counts as 0.
+ *
+ *   dtype              LITEVLM_F32 or LITEVLM_BF16 (q and o)
+ *   B, Hq, Hkv, D      batch, heads (Hq % Hkv == 0), head dim (64 or 128)
+ *   cap                the cache's positions
+ *   max_q              host upper bound on every m_b (0..LITEVLM_MAX_CACHE4)
+ *   max_len            host upper bound on every n_b (0..cap). Longer segments are
+ *                      cut to the bounds (undefined values, no out-of-range access).
+ *   weight_rows        leading queries of each sample that add weight (0..max_q)
+ *   q                  dev [total, Hq, D], total = cu_q[B]
+ *   cu_q               dev int32 [B+1], non-decreasing, cu_q[0] = 0
+ *   lengths            dev int32 [B]
+ *   softmax_scale      finite, > 0
+ *   o                  dev out [total, Hq, D]; rows past total are untouched
+ *   weight_in          dev fp32 [B, Hkv, cap], or NULL = 0 (ignored when weight_rows is 0)
+ *   weight_out         dev out fp32 [B, Hkv, cap], required when weight_rows > 0 (may be
+ *                      weight_in): written for j < n_b, untouched behind
+ *   workspace          dev scratch of litevlm_cache4_attn_workspace() bytes; contents on
+ *                      entry are ignored, and calls that may run concurrently must not
+ *                      share one
+ */
+litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t cap,
+                                     int32_t max_q, int32_t max_len, int32_t weight_rows, const void* q,
+                                     const int32_t* cu_q, const void* cache, const int32_t* lengths,
+                                     float softmax_scale, void* o, const float* weight_in, float* weight_out,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * litevlm_cache4_evict - keeps the rows of largest accumulated attention weight.
+ *
+ * Paper: Design section, Token Selection Module paragraph, and Related Work,
+ * Visual Token Compression (tokens kept by the attention they receive), applied
+ * to the cache while tokens are generated.
+ *
+ * Per sample b and KV head g, n_b = lengths[b]: where n_b <= budget every row is
+ * kept; else the last `recent` rows, and of the others the (budget - recent) of
+ * largest weight[b,g,j] (exactly equal weights keep the lower position; a NaN
+ * counts as larger than any number). The kept rows move to positions
+ * 0..lengths_out[b]-1 of the new cache in their order, with their weights;
+ * lengths_out[b] = min(n_b, budget), for every head alike.
+ *
+ *   B, Hkv, D          batch, KV heads (1..LITEVLM_MAX_HEADS), head dim (64 or 128)
+ *   cap, cap_out       positions of the cache and of the new one (budget <= cap_out)
+ *   max_len            host upper bound on every n_b (0..cap); longer ones are cut to it
+ *   budget, recent     rows to keep (1..LITEVLM_MAX_CACHE4), of them the newest ones (0..budget)
+ *   cache, weight      dev, the 4-bit cache and fp32 [B, Hkv, cap]
+ *   lengths            dev int32 [B]
+ *   cache_out          dev out, a 4-bit cache of cap_out positions
+ *   weight_out         dev out fp32 [B, Hkv, cap_out]
+ *   lengths_out        dev out int32 [B]
+ *   kept_index         dev out int32 [B, Hkv, budget]: each kept row's former position,
+ *                      ascending; entries past lengths_out[b] are untouched, as are the
+ *                      new cache's rows and weights there
+ * No output may overlap an input (LITEVLM_ERR_BAD_VALUE).
+ */
+litevlm_status_t litevlm_cache4_evict(int32_t B, int32_t Hkv, int32_t D, int32_t cap, int32_t cap_out,
+                                      int32_t max_len, int32_t budget, int32_t recent, const void* cache,
+                                      const float* weight, const int32_t* lengths, void* cache_out,
+                                      float* weight_out, int32_t* lengths_out, int32_t* kept_index,
+                                      void* stream);
+
+/* Most drafted tokens of a sample that litevlm_verify_draft takes. */
+#define LITEVLM_MAX_DRAFT 64
+
+/* Bytes of device workspace litevlm_verify_draft needs (0 when the sizes are invalid). */
+size_t litevlm_verify_draft_workspace(int32_t B, int32_t max_draft, int32_t V);
+
+/*
+ * litevlm_verify_draft - accepts or refuses drafted tokens against the target's
+ * probabilities, from given random numbers, and draws the token that follows.
+ *
+ * Paper: Design section, speculative decoding paragraph (candidates of a draft
+ * model verified in one pass with the KV cache).
+ *
+ * Sample b has n = n_draft[b] drafted tokens x_0..x_{n-1} (clamped to
+ * 0..max_draft). Token i is accepted while u[b,i] * q_i(x_i) < p_i(x_i), p_i =
+ * target[b,i], q_i = proposal[b,i]; the product is exact. With a the accepted
+ * ones in front of the first refusal, the token that follows them is drawn from
+ *   w(v) = max(p_a(v) - q_a(v), 0)   if a < n,   w(v) = p_a(v)   if a = n:
+ * the first v with w(v) > 0 and sum_{v' <= v} w(v') > r[b] * sum w, in 64 bits
+ * (the last v with w(v) > 0 if there is none, as for r >= 1). Where the
+ * difference leaves nothing, w = p_a; where that is empty too, the token is -1.
+ * Weights that are NaN, infinite or negative count as 0, a comparison with a NaN
+ * refuses, and so does a token outside [0, V).
+ *
+ *   dtype              LITEVLM_F32 or LITEVLM_BF16 (target, proposal)
+ *   B, max_draft, V    batch (1..LITEVLM_MAX_BATCH), drafted tokens at most
+ *                      (1..LITEVLM_MAX_DRAFT), vocabulary (1..16777216)
+ *   draft              dev int32 [B, max_draft]
+ *   n_draft            dev int32 [B], or NULL = max_draft
+ *   target             dev [B, max_draft + 1, V]: p_i, of the token that follows i drafts
+ *   proposal           dev [B, max_draft, V]: q_i, or NULL: the drafts were not drawn
+ *                      (q_i(x_i) = 1, 0 elsewhere)
+ *   u, r               dev fp32 [B, max_draft], [B]: uniform numbers in [0, 1)
+ *   lengths            dev int32 [B] or NULL: cached rows of each sample, those of its n
+ *                      drafts included
+ *   tokens             dev out int32 [B, max_draft + 1]: the accepted drafts, the drawn
+ *                      token, then -1
+ *   n_accepted         dev out int32 [B]: a
+ *   lengths_out        dev out int32 [B], required with lengths (may be the same):
+ *                      lengths[b] - (n - a), the rows that stay valid
+ *   workspace          dev scratch of litevlm_verify_draft_workspace() bytes (contents on
+ *                      entry ignored; calls that may run concurrently must not share one)
+ */
+litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draft, int32_t V,
+                                      const int32_t* draft, const int32_t* n_draft, const void* target,
+                                      const void* proposal, const float* u, const float* r,
+                                      const int32_t* lengths, int32_t* tokens, int32_t* n_accepted,
+                                      int32_t* lengths_out, void* workspace, size_t workspace_bytes,
+                                      void* stream);
 
 #ifdef __cplusplus
 }

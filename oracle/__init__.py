@@ -27,3 +27,4 @@ from .litevlm import (  # noqa: F401
 )
 from . import tsm  # noqa: F401,E402  (the Token Selection Module front end)
 from . import psm  # noqa: F401,E402  (the Patch Selection Module forward pass)
+from . import cache4  # noqa: F401,E402  (the 4-bit cache, draft verification)

@@ -11,6 +11,11 @@ the path runs in the library's HIP kernels:
     prefill_attn(...)      causal GQA prefill attention over the packed sequence
     decode_attn(...)       extend-one decode attention over the compacted KV cache
     tsm_qk(...)            the Token Selection Module's scoring q and k from hidden states
+    cache4_append(...)     rows of K and V into a cache held in 4 bits (cache4_empty makes one,
+                           cache4_read reads rows back)
+    cache4_attn(...)       attention of each sample's newest tokens over that cache
+    cache4_evict(...)      its rows of largest accumulated attention weight, in a new cache
+    verify_draft(...)      drafted tokens against the target's probabilities
 """
 from __future__ import annotations
 
@@ -24,7 +29,8 @@ from . import _abi
 from ._abi import LiteVLMError, load  # noqa: F401
 
 __all__ = ["patch_select", "token_score_topk", "select_score_topk", "prefill_attn", "decode_attn", "tsm_qk", "tsm_fold_gain",
-           "gather_hidden", "psm_forward",
+           "gather_hidden", "psm_forward", "cache4_empty", "cache4_append", "cache4_read", "cache4_attn",
+           "cache4_attn_workspace_bytes", "cache4_evict", "verify_draft", "verify_draft_workspace_bytes",
            "dtype_code",
            "workspace_bytes", "decode_workspace_bytes", "LiteVLMError", "load"]
 
@@ -299,4 +305,203 @@ def psm_forward(emb: torch.Tensor, params: torch.Tensor, n_heads: int, d_ff: int
                                  params.numel(), _ptr(o), _ptr(workspace),
                                  workspace.numel() * workspace.element_size(), _stream(dev))
     _abi.check(st, "litevlm_psm_forward")
+    return o
+
+
+# ------------------------------------------------------------------ the 4-bit cache, drafted tokens
+
+def _arg(name: str, t: torch.Tensor, dtype, shape: tuple, device) -> int:
+    """Address of an argument that has this type, shape and device, densely laid out."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _enqueue(call: str, device, *args) -> None:
+    """Runs a call on the current stream of `device`, which need not be the current one."""
+    if device.type != "cuda":
+        raise ValueError(f"{call}: tensors must live on the GPU")
+    fn = getattr(load(), call)
+    if device.index == torch.cuda.current_device():
+        st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if st:
+        _abi.check(st, call)
+
+
+def _float_code(name: str, t: torch.Tensor) -> int:
+    if t.dtype is torch.bfloat16:
+        return _abi.BF16
+    if t.dtype is torch.float32:
+        return _abi.F32
+    raise TypeError(f"{name}: float32 or bfloat16 expected, got {t.dtype}")
+
+
+def _cache_shape(cache: torch.Tensor, D: int):
+    """(B, Hkv, cap) of a cache tensor of head dim D, and its address."""
+    if D not in (64, 128):
+        raise ValueError(f"head dim {D}: 64 or 128 expected")
+    B, Hkv, n = cache.shape
+    cap, rest = divmod(n, D + D // 16)
+    if rest:
+        raise ValueError(f"a cache of head dim {D} has {D + D // 16} bytes a position, not {n} for all of them")
+    return B, Hkv, cap, _arg("cache", cache, torch.uint8, (B, Hkv, n), cache.device)
+
+
+def cache4_empty(B: int, Hkv: int, D: int, cap: int, device="cuda") -> torch.Tensor:
+    """A 4-bit cache of `cap` positions (a multiple of 32) for each sample and KV head: uint8
+    [B, Hkv, cap * (D + D/16)], laid out as include/litevlm.h says; every value is 0."""
+    n = int(load().litevlm_cache4_bytes(B, Hkv, D, cap))
+    if n == 0:
+        raise ValueError(f"no 4-bit cache for B={B} Hkv={Hkv} D={D} cap={cap}")
+    return torch.zeros((B, Hkv, n // (B * Hkv)), dtype=torch.uint8, device=device)
+
+
+def cache4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_new: torch.Tensor, start: torch.Tensor,
+                  max_new: int, weight: Optional[torch.Tensor] = None) -> None:
+    """Quantises packed rows k, v [rows,Hkv,D] (fp32 or bf16) into the cache: rows cu_new[b].. of
+    sample b go to positions start[b].. (at most max_new a sample). weight [B,Hkv,cap] is set to
+    0 at those positions."""
+    rows, _, D = k.shape
+    dev = k.device
+    B, Hkv, cap, cptr = _cache_shape(cache, D)
+    shape = (rows, Hkv, D)
+    _enqueue("litevlm_cache4_append", dev, _float_code("k", k), B, Hkv, D, cap, max_new,
+             _arg("k", k, k.dtype, shape, cache.device), _arg("v", v, k.dtype, shape, dev),
+             _arg("cu_new", cu_new, torch.int32, (B + 1,), dev), _arg("start", start, torch.int32, (B,), dev), cptr,
+             None if weight is None else _arg("weight", weight, torch.float32, (B, Hkv, cap), dev))
+
+
+def cache4_read(cache: torch.Tensor, D: int, cu_rows: torch.Tensor, start: torch.Tensor, max_rows: int,
+                rows: Optional[int] = None, dtype: torch.dtype = torch.bfloat16, out: Optional[tuple] = None):
+    """The values of cached rows: rows cu_rows[b].. of the packed result are positions start[b]..
+    of sample b. Returns (k, v) [rows,Hkv,D]; without `out` they have `rows` rows (B * max_rows by
+    default) of `dtype`, and rows past cu_rows[B] are not written."""
+    B, Hkv, cap, cptr = _cache_shape(cache, D)
+    dev = cache.device
+    if out is None:
+        shape = (B * max_rows if rows is None else rows, Hkv, D)
+        out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
+    k, v = out
+    shape = (k.shape[0], Hkv, D)
+    _enqueue("litevlm_cache4_read", dev, _float_code("k", k), B, Hkv, D, cap, max_rows, cptr,
+             _arg("start", start, torch.int32, (B,), dev), _arg("cu_rows", cu_rows, torch.int32, (B + 1,), dev),
+             _arg("k", k, k.dtype, shape, dev), _arg("v", v, k.dtype, shape, dev))
+    return k, v
+
+
+def cache4_attn_workspace_bytes(dtype: torch.dtype, B: int, Hq: int, Hkv: int, D: int, max_q: int, max_len: int,
+                                weight_rows: int = 0) -> int:
+    return int(load().litevlm_cache4_attn_workspace(dtype_code(dtype), B, Hq, Hkv, D, max_q, max_len, weight_rows))
+
+
+def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, lengths: torch.Tensor, max_q: int,
+                max_len: int, softmax_scale: Optional[float] = None, weight: Optional[torch.Tensor] = None,
+                weight_out: Optional[torch.Tensor] = None, weight_rows: int = 0, out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the packed queries q [rows,Hq,D] (fp32 or bf16; those of sample b are its newest
+    tokens, whose keys and values are in the cache) over the first lengths[b] cached rows. With
+    weight_rows > 0, weight_out [B,Hkv,cap] = weight + the attention that each row receives from
+    each sample's first weight_rows queries (weight None: 0; weight_out None: in place).
+    Returns [rows,Hq,D] in q's type."""
+    rows, Hq, D = q.shape
+    dev = q.device
+    B, Hkv, cap, cptr = _cache_shape(cache, D)
+    if cache.device != dev:
+        raise ValueError(f"the cache lives on {cache.device}, the queries on {dev}")
+    code = _float_code("q", q)
+    if softmax_scale is None:
+        softmax_scale = 1.0 / math.sqrt(D)
+    if out is None:
+        out = torch.empty_like(q)
+    win = wout = None
+    if weight_rows:
+        if weight is not None:
+            win = _arg("weight", weight, torch.float32, (B, Hkv, cap), dev)
+        if weight_out is None:
+            if weight is None:
+                raise ValueError("weight_rows > 0 needs weight or weight_out")
+            wout = win
+        else:
+            wout = _arg("weight_out", weight_out, torch.float32, (B, Hkv, cap), dev)
+    if workspace is None:
+        n = load().litevlm_cache4_attn_workspace(code, B, Hq, Hkv, D, max_q, max_len, weight_rows)
+        workspace = torch.empty((n or 1,), dtype=torch.uint8, device=dev)
+    _enqueue("litevlm_cache4_attn", dev, code, B, Hq, Hkv, D, cap, max_q, max_len, weight_rows,
+             _arg("q", q, q.dtype, (rows, Hq, D), dev), _arg("cu_q", cu_q, torch.int32, (B + 1,), dev), cptr,
+             _arg("lengths", lengths, torch.int32, (B,), dev), softmax_scale,
+             _arg("out", out, q.dtype, (rows, Hq, D), dev), win, wout, _ptr(workspace), workspace.nbytes)
+    return out
+
+
+def cache4_evict(cache: torch.Tensor, D: int, weight: torch.Tensor, lengths: torch.Tensor, budget: int, recent: int,
+                 max_len: int, cap_out: Optional[int] = None, out: Optional[dict] = None) -> dict:
+    """Keeps at most `budget` rows of each sample and KV head: the last `recent` ones and those of
+    largest weight [B,Hkv,cap]. Returns a dict of new tensors: cache (of cap_out positions, by
+    default budget rounded up to 32), weight [B,Hkv,cap_out], lengths [B] and kept_index
+    [B,Hkv,budget], all valid up to lengths[b]. ``out`` may supply them under the same keys."""
+    B, Hkv, cap, cptr = _cache_shape(cache, D)
+    dev = cache.device
+    o = dict(out or {})
+    if "cache" not in o:
+        o["cache"] = cache4_empty(B, Hkv, D, (budget + 31) // 32 * 32 if cap_out is None else cap_out, dev)
+    B2, H2, cap_out, optr = _cache_shape(o["cache"], D)
+    if (B2, H2) != (B, Hkv):
+        raise ValueError(f"the new cache is for {B2} samples and {H2} heads, not {B} and {Hkv}")
+    if "weight" not in o:
+        o["weight"] = torch.empty((B, Hkv, cap_out), dtype=torch.float32, device=dev)
+    if "lengths" not in o:
+        o["lengths"] = torch.empty((B,), dtype=torch.int32, device=dev)
+    if "kept_index" not in o:
+        o["kept_index"] = torch.empty((B, Hkv, budget), dtype=torch.int32, device=dev)
+    _enqueue("litevlm_cache4_evict", dev, B, Hkv, D, cap, cap_out, max_len, budget, recent, cptr,
+             _arg("weight", weight, torch.float32, (B, Hkv, cap), dev),
+             _arg("lengths", lengths, torch.int32, (B,), dev), optr,
+             _arg("out weight", o["weight"], torch.float32, (B, Hkv, cap_out), dev),
+             _arg("out lengths", o["lengths"], torch.int32, (B,), dev),
+             _arg("out kept_index", o["kept_index"], torch.int32, (B, Hkv, budget), dev))
+    return o
+
+
+def verify_draft_workspace_bytes(B: int, max_draft: int, V: int) -> int:
+    return int(load().litevlm_verify_draft_workspace(B, max_draft, V))
+
+
+def verify_draft(draft: torch.Tensor, target: torch.Tensor, proposal: Optional[torch.Tensor], u: torch.Tensor,
+                 r: torch.Tensor, n_draft: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                 out: Optional[dict] = None, workspace: Optional[torch.Tensor] = None) -> dict:
+    """Drafted tokens draft [B,m] (int32) against target probabilities [B,m+1,V] (fp32 or bf16) and
+    the draft model's [B,m,V] (None: the drafts were not drawn), with uniform numbers u [B,m] and
+    r [B]. Returns a dict: tokens [B,m+1] (the accepted drafts, one drawn token, then -1),
+    n_accepted [B] and, with `lengths`, lengths [B] without the refused drafts' rows. ``out`` may
+    supply them under the same keys."""
+    B, m = draft.shape
+    V = target.shape[2]
+    dev = draft.device
+    code = _float_code("target", target)
+    o = dict(out or {})
+    if "tokens" not in o:
+        o["tokens"] = torch.empty((B, m + 1), dtype=torch.int32, device=dev)
+    if "n_accepted" not in o:
+        o["n_accepted"] = torch.empty((B,), dtype=torch.int32, device=dev)
+    lin = lout = None
+    if lengths is not None:
+        lin = _arg("lengths", lengths, torch.int32, (B,), dev)
+        if "lengths" not in o:
+            o["lengths"] = torch.empty((B,), dtype=torch.int32, device=dev)
+        lout = _arg("out lengths", o["lengths"], torch.int32, (B,), dev)
+    if workspace is None:
+        n = load().litevlm_verify_draft_workspace(B, m, V)
+        workspace = torch.empty((n or 1,), dtype=torch.uint8, device=dev)
+    _enqueue("litevlm_verify_draft", dev, code, B, m, V, _arg("draft", draft, torch.int32, (B, m), dev),
+             None if n_draft is None else _arg("n_draft", n_draft, torch.int32, (B,), dev),
+             _arg("target", target, target.dtype, (B, m + 1, V), dev),
+             None if proposal is None else _arg("proposal", proposal, target.dtype, (B, m, V), dev),
+             _arg("u", u, torch.float32, (B, m), dev), _arg("r", r, torch.float32, (B,), dev), lin,
+             _arg("out tokens", o["tokens"], torch.int32, (B, m + 1), dev),
+             _arg("out n_accepted", o["n_accepted"], torch.int32, (B,), dev), lout, _ptr(workspace),
+             workspace.nbytes)
     return o

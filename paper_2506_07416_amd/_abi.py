@@ -17,6 +17,8 @@ F32, BF16, FP8_E4M3 = 0, 1, 2
 MAX_VIEWS, MAX_VISUAL, MAX_BATCH, MAX_HEADS = 64, 16384, 256, 128
 NOALLOC_SCRATCH_BYTES = 8 << 20
 MAX_FUSED_VIEWS = 8
+MAX_CACHE4 = 16777216
+MAX_DRAFT = 64
 
 # Every symbol the header declares, with its C signature.
 _vp, _i32, _f32, _f64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_double, ctypes.c_size_t
@@ -50,6 +52,17 @@ SIGNATURES = {
     "litevlm_decode_attn_workspace": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32]),
     "litevlm_decode_attn": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
                                    _i32, _f32, _f32, _f32, _f32, _vp, _vp, _sz, _vp]),
+    "litevlm_cache4_bytes": (_sz, [_i32, _i32, _i32, _i32]),
+    "litevlm_cache4_append": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "litevlm_cache4_read": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "litevlm_cache4_attn_workspace": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32]),
+    "litevlm_cache4_attn": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _f32,
+                                   _vp, _vp, _vp, _vp, _sz, _vp]),
+    "litevlm_cache4_evict": (_i32, [_i32, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                    _vp, _vp]),
+    "litevlm_verify_draft_workspace": (_sz, [_i32, _i32, _i32]),
+    "litevlm_verify_draft": (_i32, [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                    _sz, _vp]),
 }
 
 _LIB = None

@@ -502,3 +502,244 @@ litevlm_status_t litevlm_tsm_qk(int32_t B, int32_t S, int32_t V_full, int32_t Dm
 }
 
 }  // extern "C"
+
+namespace {
+
+litevlm_status_t check_cache4(int32_t B, int32_t Hkv, int32_t D, int32_t cap) {
+  if (B < 1 || B > LITEVLM_MAX_BATCH || Hkv < 1 || Hkv > LITEVLM_MAX_HEADS || (D != 64 && D != 128))
+    return LITEVLM_ERR_BAD_SHAPE;
+  if (cap < 32 || cap % 32 != 0 || cap > LITEVLM_MAX_CACHE4) return LITEVLM_ERR_BAD_SHAPE;
+  return LITEVLM_OK;
+}
+
+litevlm_status_t check_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t max_q,
+                                   int32_t max_len, int32_t weight_rows) {
+  if (dtype != LITEVLM_F32 && dtype != LITEVLM_BF16) return LITEVLM_ERR_UNSUPPORTED;
+  if (B < 1 || B > LITEVLM_MAX_BATCH || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || Hq > LITEVLM_MAX_HEADS ||
+      (D != 64 && D != 128))
+    return LITEVLM_ERR_BAD_SHAPE;
+  if (max_q < 0 || max_q > LITEVLM_MAX_CACHE4 || max_len < 0 || max_len > LITEVLM_MAX_CACHE4)
+    return LITEVLM_ERR_BAD_SHAPE;
+  // packed rows are counted in an int, and so are the rows of a KV head
+  if ((int64_t)B * max_q > INT32_MAX / 2 || (int64_t)max_q * (Hq / Hkv) > INT32_MAX / 2) return LITEVLM_ERR_BAD_SHAPE;
+  if (weight_rows < 0 || weight_rows > max_q) return LITEVLM_ERR_BAD_VALUE;
+  return LITEVLM_OK;
+}
+
+// Arguments that append and read share.
+litevlm_status_t check_cache4_rows(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap, int32_t max_rows,
+                                   const void* k, const void* v, const int32_t* cu, const int32_t* start,
+                                   const void* cache) {
+  if (!k || !v || !cu || !start || !cache) return LITEVLM_ERR_NULL_POINTER;
+  if (dtype != LITEVLM_F32 && dtype != LITEVLM_BF16) return LITEVLM_ERR_UNSUPPORTED;
+  const litevlm_status_t sh = check_cache4(B, Hkv, D, cap);
+  if (sh != LITEVLM_OK) return sh;
+  if (max_rows < 0 || max_rows > cap || (int64_t)B * max_rows > INT32_MAX / 2) return LITEVLM_ERR_BAD_SHAPE;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(cache, 16) || !aligned(cu, 4) || !aligned(start, 4))
+    return LITEVLM_ERR_MISALIGNED;
+  return LITEVLM_OK;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t litevlm_cache4_bytes(int32_t B, int32_t Hkv, int32_t D, int32_t cap) {
+  if (check_cache4(B, Hkv, D, cap) != LITEVLM_OK) return 0;
+  return (size_t)B * Hkv * cap * (D + D / 16);
+}
+
+litevlm_status_t litevlm_cache4_append(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap,
+                                       int32_t max_new, const void* k, const void* v, const int32_t* cu_new,
+                                       const int32_t* start, void* cache, float* weight, void* stream) {
+  const litevlm_status_t st = check_cache4_rows(dtype, B, Hkv, D, cap, max_new, k, v, cu_new, start, cache);
+  if (st != LITEVLM_OK) return st;
+  if (weight && !aligned(weight, 4)) return LITEVLM_ERR_MISALIGNED;
+  Cache4RowsArgs a{};
+  a.dtype = dtype;
+  a.B = B;
+  a.Hkv = Hkv;
+  a.D = D;
+  a.cap = cap;
+  a.max_rows = max_new;
+  a.k_in = k;
+  a.v_in = v;
+  a.cu = cu_new;
+  a.start = start;
+  a.cache = cache;
+  a.weight = weight;
+  return hip_status(launch_cache4_append(a, static_cast<hipStream_t>(stream)));
+}
+
+litevlm_status_t litevlm_cache4_read(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap,
+                                     int32_t max_rows, const void* cache, const int32_t* start,
+                                     const int32_t* cu_rows, void* k, void* v, void* stream) {
+  const litevlm_status_t st = check_cache4_rows(dtype, B, Hkv, D, cap, max_rows, k, v, cu_rows, start, cache);
+  if (st != LITEVLM_OK) return st;
+  Cache4RowsArgs a{};
+  a.dtype = dtype;
+  a.B = B;
+  a.Hkv = Hkv;
+  a.D = D;
+  a.cap = cap;
+  a.max_rows = max_rows;
+  a.k_out = k;
+  a.v_out = v;
+  a.cu = cu_rows;
+  a.start = start;
+  a.cache = const_cast<void*>(cache);
+  return hip_status(launch_cache4_read(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+                                     int32_t max_q, int32_t max_len, int32_t weight_rows) {
+  if (check_cache4_attn(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows) != LITEVLM_OK) return 0;
+  return cache4_attn_layout(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows).total;
+}
+
+litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t cap,
+                                     int32_t max_q, int32_t max_len, int32_t weight_rows, const void* q,
+                                     const int32_t* cu_q, const void* cache, const int32_t* lengths,
+                                     float softmax_scale, void* o, const float* weight_in, float* weight_out,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  if (!q || !cu_q || !cache || !lengths || !o) return LITEVLM_ERR_NULL_POINTER;
+  litevlm_status_t st = check_cache4_attn(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows);
+  if (st != LITEVLM_OK) return st;
+  st = check_cache4(B, Hkv, D, cap);
+  if (st != LITEVLM_OK) return st;
+  if (max_len > cap) return LITEVLM_ERR_BAD_SHAPE;
+  if (weight_rows > 0 && !weight_out) return LITEVLM_ERR_NULL_POINTER;
+  if (!finite_pos(softmax_scale)) return LITEVLM_ERR_BAD_VALUE;
+  const void* big[] = {q, cache, o, workspace};
+  for (const void* p : big)
+    if (p && !aligned(p, 16)) return LITEVLM_ERR_MISALIGNED;
+  const void* small[] = {cu_q, lengths, weight_in, weight_out};
+  for (const void* p : small)
+    if (p && !aligned(p, 4)) return LITEVLM_ERR_MISALIGNED;
+  const size_t need = cache4_attn_layout(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows).total;
+  if (!workspace || workspace_bytes < need) return LITEVLM_ERR_WORKSPACE;
+  Cache4AttnArgs a;
+  a.dtype = dtype;
+  a.B = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.D = D;
+  a.cap = cap;
+  a.max_q = max_q;
+  a.max_len = max_len;
+  a.weight_rows = weight_rows;
+  a.q = q;
+  a.cu_q = cu_q;
+  a.cache = cache;
+  a.lengths = lengths;
+  a.scale_log2 = (float)((double)softmax_scale * 1.4426950408889634);
+  a.o = o;
+  a.weight_in = weight_in;
+  a.weight_out = weight_out;
+  a.workspace = workspace;
+  return hip_status(launch_cache4_attn(a, static_cast<hipStream_t>(stream)));
+}
+
+litevlm_status_t litevlm_cache4_evict(int32_t B, int32_t Hkv, int32_t D, int32_t cap, int32_t cap_out,
+                                      int32_t max_len, int32_t budget, int32_t recent, const void* cache,
+                                      const float* weight, const int32_t* lengths, void* cache_out,
+                                      float* weight_out, int32_t* lengths_out, int32_t* kept_index,
+                                      void* stream) {
+  if (!cache || !weight || !lengths || !cache_out || !weight_out || !lengths_out || !kept_index)
+    return LITEVLM_ERR_NULL_POINTER;
+  litevlm_status_t st = check_cache4(B, Hkv, D, cap);
+  if (st == LITEVLM_OK) st = check_cache4(B, Hkv, D, cap_out);
+  if (st != LITEVLM_OK) return st;
+  if (max_len < 0 || max_len > cap || budget < 1 || budget > cap_out) return LITEVLM_ERR_BAD_SHAPE;
+  if (recent < 0 || recent > budget) return LITEVLM_ERR_BAD_VALUE;
+  if (!aligned(cache, 16) || !aligned(cache_out, 16) || !aligned(weight, 4) || !aligned(weight_out, 4) ||
+      !aligned(lengths, 4) || !aligned(lengths_out, 4) || !aligned(kept_index, 4))
+    return LITEVLM_ERR_MISALIGNED;
+  const size_t heads = (size_t)B * Hkv;
+  const struct {
+    const void* p;
+    size_t n;
+  } in[] = {{cache, litevlm_cache4_bytes(B, Hkv, D, cap)}, {weight, heads * cap * 4}, {lengths, (size_t)B * 4}},
+    out[] = {{cache_out, litevlm_cache4_bytes(B, Hkv, D, cap_out)},
+             {weight_out, heads * cap_out * 4},
+             {lengths_out, (size_t)B * 4},
+             {kept_index, heads * budget * 4}};
+  for (int i = 0; i < 4; ++i) {
+    for (const auto& x : in)
+      if (overlap(x.p, x.n, out[i].p, out[i].n)) return LITEVLM_ERR_BAD_VALUE;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[j].p, out[j].n, out[i].p, out[i].n)) return LITEVLM_ERR_BAD_VALUE;
+  }
+  Cache4EvictArgs a;
+  a.B = B;
+  a.Hkv = Hkv;
+  a.D = D;
+  a.cap = cap;
+  a.cap_out = cap_out;
+  a.max_len = max_len;
+  a.budget = budget;
+  a.recent = recent;
+  a.cache = cache;
+  a.weight = weight;
+  a.lengths = lengths;
+  a.cache_out = cache_out;
+  a.weight_out = weight_out;
+  a.lengths_out = lengths_out;
+  a.kept_index = kept_index;
+  return hip_status(launch_cache4_evict(a, static_cast<hipStream_t>(stream)));
+}
+
+static litevlm_status_t check_verify_shape(int32_t B, int32_t max_draft, int32_t V) {
+  if (B < 1 || B > LITEVLM_MAX_BATCH || max_draft < 1 || max_draft > LITEVLM_MAX_DRAFT || V < 1 || V > (1 << 24))
+    return LITEVLM_ERR_BAD_SHAPE;
+  return LITEVLM_OK;
+}
+
+size_t litevlm_verify_draft_workspace(int32_t B, int32_t max_draft, int32_t V) {
+  if (check_verify_shape(B, max_draft, V) != LITEVLM_OK) return 0;
+  return verify_layout(B, V).total;
+}
+
+litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draft, int32_t V,
+                                      const int32_t* draft, const int32_t* n_draft, const void* target,
+                                      const void* proposal, const float* u, const float* r,
+                                      const int32_t* lengths, int32_t* tokens, int32_t* n_accepted,
+                                      int32_t* lengths_out, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+  if (!draft || !target || !u || !r || !tokens || !n_accepted || (lengths && !lengths_out))
+    return LITEVLM_ERR_NULL_POINTER;
+  if (dtype != LITEVLM_F32 && dtype != LITEVLM_BF16) return LITEVLM_ERR_UNSUPPORTED;
+  const litevlm_status_t sh = check_verify_shape(B, max_draft, V);
+  if (sh != LITEVLM_OK) return sh;
+  const void* big[] = {target, proposal, workspace};
+  for (const void* p : big)
+    if (p && !aligned(p, 16)) return LITEVLM_ERR_MISALIGNED;
+  const void* small[] = {draft, n_draft, u, r, lengths, tokens, n_accepted, lengths_out};
+  for (const void* p : small)
+    if (p && !aligned(p, 4)) return LITEVLM_ERR_MISALIGNED;
+  if (!workspace || workspace_bytes < verify_layout(B, V).total) return LITEVLM_ERR_WORKSPACE;
+  VerifyArgs a;
+  a.dtype = dtype;
+  a.B = B;
+  a.max_draft = max_draft;
+  a.V = V;
+  a.draft = draft;
+  a.n_draft = n_draft;
+  a.target = target;
+  a.proposal = proposal;
+  a.u = u;
+  a.r = r;
+  a.lengths = lengths;
+  a.tokens = tokens;
+  a.n_accepted = n_accepted;
+  a.lengths_out = lengths_out;
+  a.workspace = workspace;
+  return hip_status(launch_verify_draft(a, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/litevlm.h"
 #include "viewsel.hpp"
 
@@ -129,6 +131,79 @@ struct PsmArgs {
   void* workspace;
 };
 hipError_t launch_psm_forward(const PsmArgs& a, hipStream_t stream);
+
+// Rows of K and V into (k_in, v_in) or out of (k_out, v_out) the 4-bit cache.
+struct Cache4RowsArgs {
+  int dtype, B, Hkv, D, cap, max_rows;
+  const void* k_in;
+  const void* v_in;
+  void* k_out;
+  void* v_out;
+  const int32_t* cu;
+  const int32_t* start;
+  void* cache;
+  float* weight;
+};
+hipError_t launch_cache4_append(const Cache4RowsArgs& a, hipStream_t stream);
+hipError_t launch_cache4_read(const Cache4RowsArgs& a, hipStream_t stream);
+
+// Workspace of the attention over the 4-bit cache.
+struct Cache4AttnLayout {
+  size_t total;
+};
+Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, int max_q, int max_len,
+                                    int weight_rows);
+
+struct Cache4AttnArgs {
+  int dtype, B, Hq, Hkv, D, cap, max_q, max_len, weight_rows;
+  const void* q;
+  const int32_t* cu_q;
+  const void* cache;
+  const int32_t* lengths;
+  float scale_log2;  // softmax_scale*log2(e)
+  void* o;
+  const float* weight_in;
+  float* weight_out;
+  void* workspace;
+};
+hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream);
+
+struct Cache4EvictArgs {
+  int B, Hkv, D, cap, cap_out, max_len, budget, recent;
+  const void* cache;
+  const float* weight;
+  const int32_t* lengths;
+  void* cache_out;
+  float* weight_out;
+  int32_t* lengths_out;
+  int32_t* kept_index;
+};
+hipError_t launch_cache4_evict(const Cache4EvictArgs& a, hipStream_t stream);
+
+// Workspace of the draft verification: per (sample, chunk of the vocabulary) two
+// sums in 64 bits.
+struct VerifyLayout {
+  int chunks;
+  size_t total;
+};
+VerifyLayout verify_layout(int B, int V);
+
+struct VerifyArgs {
+  int dtype, B, max_draft, V;
+  const int32_t* draft;
+  const int32_t* n_draft;
+  const void* target;
+  const void* proposal;
+  const float* u;
+  const float* r;
+  const int32_t* lengths;
+  int32_t* tokens;
+  int32_t* n_accepted;
+  int32_t* lengths_out;
+  void* workspace;
+};
+hipError_t launch_verify_draft(const VerifyArgs& a, hipStream_t stream);
+
 hipError_t launch_tsm_fold_gain(const void* w, const float* gamma, void* w_out, int rows, int cols,
                                 hipStream_t stream);
 
