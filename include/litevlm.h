@@ -578,7 +578,7 @@ size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32
  *   dtype              LITEVLM_F32 or LITEVLM_BF16 (q and o)
  *   B, Hq, Hkv, D      batch, heads (Hq % Hkv == 0), head dim (64 or 128)
  *   cap                the cache's positions
- *   max_q              host upper bound on every m_b (0..LITEVLM_MAX_CACHE4)
+ *   max_q              host upper bound on every m_b (max_q * Hq <= 2^26)
  *   max_len            host upper bound on every n_b (0..cap). Longer segments are
  *                      cut to the bounds (undefined values, no out-of-range access).
  *   weight_rows        leading queries of each sample that add weight (0..max_q)

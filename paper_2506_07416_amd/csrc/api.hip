@@ -520,8 +520,8 @@ litevlm_status_t check_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32_t
     return LITEVLM_ERR_BAD_SHAPE;
   if (max_q < 0 || max_q > LITEVLM_MAX_CACHE4 || max_len < 0 || max_len > LITEVLM_MAX_CACHE4)
     return LITEVLM_ERR_BAD_SHAPE;
-  // packed rows are counted in an int, and so are the rows of a KV head
-  if ((int64_t)B * max_q > INT32_MAX / 2 || (int64_t)max_q * (Hq / Hkv) > INT32_MAX / 2) return LITEVLM_ERR_BAD_SHAPE;
+  // packed rows are counted in an int, and the grid over the rows of a sample must fit
+  if ((int64_t)B * max_q > INT32_MAX / 2 || (int64_t)max_q * Hq > ((int64_t)1 << 26)) return LITEVLM_ERR_BAD_SHAPE;
   if (weight_rows < 0 || weight_rows > max_q) return LITEVLM_ERR_BAD_VALUE;
   return LITEVLM_OK;
 }

@@ -24,6 +24,12 @@
 namespace litevlm {
 namespace {
 
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kKeys = 32;              // keys of a wave's step
+constexpr int kStep = kWaves * kKeys;  // keys of a workgroup's step
+constexpr int64_t kGroupsWanted = 2048;  // workgroups of the first kernel, where the keys allow
+constexpr float kSlack = 8.f;          // the running reference may lag the maximum by this (log2)
+
 struct AttnParams {
   const void* q;
   void* o;
@@ -32,8 +38,15 @@ struct AttnParams {
   const int32_t* lengths;
   const float* weight_in;
   float* weight_out;
-  float2* stat;  // [B][Hkv][G * weight_rows]: (maximum, 1 / sum) of the rows that add weight
+  float* part_o;    // [B][Hkv][rows][nsplit][D]  unnormalised outputs of the splits
+  float2* part_ml;  // [B][Hkv][rows][nsplit]     their (reference, sum)
+  float2* stat;     // [B][Hkv][weight rows]      (reference, 1 / sum) of the rows that add weight
+  float* logit;     // [B][Hkv][weight rows][lpad] their logits (log2), where they are kept
   int Hq, Hkv, G, cap, max_q, max_len, weight_rows;
+  int rows;    // max_q * G: rows of a KV head
+  int wrows;   // weight_rows * G
+  int blocks;  // row blocks
+  int nsplit, split_len, lpad;
   float scale_log2;
 };
 
@@ -52,10 +65,26 @@ __device__ __forceinline__ void split_terms(float x, __bf16* t) {
   }
 }
 
+// The rows of one sample that a workgroup or wave deals with.
+struct Sample {
+  int lo, m, rows, n;
+  __device__ __forceinline__ Sample(const AttnParams& p, int b) {
+    lo = p.cu[b];
+    m = min(p.cu[b + 1] - lo, p.max_q);
+    rows = m * p.G;
+    n = min(max(p.lengths[b], 0), p.max_len);
+  }
+  // Keys that row r sees, and the row of q and o that it is.
+  __device__ __forceinline__ int seen(const AttnParams& p, int r) const { return max(n - m + r / p.G + 1, 0); }
+  __device__ __forceinline__ int64_t qrow(const AttnParams& p, int g, int r) const {
+    return (int64_t)(lo + r / p.G) * p.Hq + g * p.G + r % p.G;
+  }
+};
+
 template <int D, int TERMS>
 struct Attn {
   static constexpr int kSteps = D / 32;  // first product: steps of a key tile
-  static constexpr int kTiles = D / 16;  // second product: tiles of the output
+  static constexpr int kTiles = D / 16;  // second product: tiles of the output, elements of a key per lane
   static constexpr bool kF32 = TERMS == 3;
 
   struct Rows {  // the queries of 16 rows, as the lane's operands
@@ -86,156 +115,370 @@ struct Attn {
     }
   }
 
-  // Logits (without the scale) of the 16 rows against the 16 keys at k0.
-  static __device__ __forceinline__ f32x4 logits(const CacheHead<D>& c, int cap, int k0, int lg, int col,
-                                                 const Rows& f) {
-    const int key = k0 + col;
-    const float scale = e8m0_scale(c.ks[(int64_t)(lg * D / 128) * cap + key]);
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(c.kc + (int64_t)key * (D / 2) + lg * (D / 8));
+  // The lane's share of 16 keys: D/8 bytes of key col and their scale.
+  struct Key {
+    uint32_t w[kSteps];
+    uint32_t scale;
+  };
+  static __device__ __forceinline__ void load_key(const CacheHead<D>& c, int cap, int k0, int lg, int col, Key& k) {
+    const uint8_t* src = c.kc + ((uint32_t)(k0 + col) * (D / 2) + lg * (D / 8));
+    if constexpr (D == 128) {
+      const uint4 x = *reinterpret_cast<const uint4*>(src);
+      k.w[0] = x.x, k.w[1] = x.y, k.w[2] = x.z, k.w[3] = x.w;
+    } else {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      k.w[0] = x.x, k.w[1] = x.y;
+    }
+    k.scale = c.ks[(uint32_t)(lg * D / 128) * (uint32_t)cap + k0 + col];
+  }
+  // Logits (without the scale) of 16 rows against those keys.
+  static __device__ __forceinline__ f32x4 logits(const bf16x8* k, const Rows& f) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < kSteps; ++t) {
-      const bf16x8 k = decode8(src[t], scale);
+    for (int t = 0; t < kSteps; ++t)
 #pragma unroll
-      for (int n = TERMS - 1; n >= 0; --n) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, f.q[t][n], s, 0, 0, 0);
-    }
+      for (int n = TERMS - 1; n >= 0; --n) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t], f.q[t][n], s, 0, 0, 0);
     return s;
+  }
+  static __device__ __forceinline__ void decode_key(const Key& k, bf16x8* out) {
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) out[t] = decode8(k.w[t], e8m0_scale(k.scale));
+  }
+
+  // The lane's share of 32 values: elements col*D/16.. of keys 16h + 4lg + i, and
+  // the scales of the four keys of each h in one word.
+  struct Value {
+    uint32_t w[8];
+    uint32_t scale[2];
+  };
+  static __device__ __forceinline__ void load_value(const CacheHead<D>& c, int cap, int k0, int lg, int col, Value& v) {
+    const uint32_t row = (uint32_t)(k0 + 4 * lg) * (D / 2) + col * (kTiles / 2);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const uint8_t* src = c.vc + (row + (16 * (kk >> 2) + (kk & 3)) * (D / 2));
+      v.w[kk] = D == 128 ? *reinterpret_cast<const uint32_t*>(src) : *reinterpret_cast<const uint16_t*>(src);
+    }
+    const uint8_t* sc = c.vs + ((uint32_t)(col * kTiles / kCacheBlock) * (uint32_t)cap + k0 + 4 * lg);
+    v.scale[0] = *reinterpret_cast<const uint32_t*>(sc);
+    v.scale[1] = *reinterpret_cast<const uint32_t*>(sc + 16);
+  }
+  // Element t of the lane's eight keys, for every t: pairs of elements of a key
+  // become pairs of keys of an element.
+  static __device__ __forceinline__ void decode_value(const Value& v, bf16x8* out) {
+    uint32_t d[8][kTiles / 2];
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const uint32_t byte = (v.scale[kk >> 2] >> (8 * (kk & 3))) & 255u;
+      const i32x4 x = __builtin_bit_cast(i32x4, decode8(v.w[kk], e8m0_scale(byte)));
+#pragma unroll
+      for (int t = 0; t < kTiles / 2; ++t) d[kk][t] = (uint32_t)x[t];
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles / 2; ++t) {
+      i32x4 even, odd;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        even[j] = (int)__builtin_amdgcn_perm(d[2 * j + 1][t], d[2 * j][t], 0x05040100u);
+        odd[j] = (int)__builtin_amdgcn_perm(d[2 * j + 1][t], d[2 * j][t], 0x07060302u);
+      }
+      out[2 * t] = __builtin_bit_cast(bf16x8, even);
+      out[2 * t + 1] = __builtin_bit_cast(bf16x8, odd);
+    }
   }
 };
 
-// One wave: 16 rows of one (sample, KV head), every key.
-template <int D, int TERMS>
-__global__ __launch_bounds__(64) void cache4_attn_kernel(AttnParams p) {
+// One workgroup: 16 * MT rows of one (sample, KV head) and the keys of one split,
+// of which wave w takes steps of 32 keys w, w + 4, ... Each wave keeps its own
+// reference, sum and output; they are joined at the end. The reference of a row
+// follows its maximum only when a logit exceeds it by kSlack: until then the
+// probabilities are at most 2^kSlack, and neither an exchange between lanes nor a
+// rescaling of the output is needed.
+template <int D, int TERMS, int MT, bool KEEP>
+__global__ __launch_bounds__(kThreads) void cache4_attn_kernel(AttnParams p) {
   using A = Attn<D, TERMS>;
-  constexpr int ET = D / 16;  // elements of a key that a lane decodes for the second product
-  const int b = blockIdx.z, g = blockIdx.y, lane = threadIdx.x, lg = lane >> 4, col = lane & 15;
-  const int lo = p.cu[b], m = min(p.cu[b + 1] - lo, p.max_q);
-  const int rows = m * p.G;
-  const int r = blockIdx.x * 16 + col;
-  if (blockIdx.x * 16 >= rows) return;
-  const int n = min(max(p.lengths[b], 0), p.max_len);
-  const bool live = r < rows;
-  const int qi = r / p.G;
-  const int64_t qrow = (int64_t)(lo + qi) * p.Hq + g * p.G + r % p.G;
-  const int seen = live ? max(n - m + qi + 1, 0) : 0;  // keys that the row sees
-  const int last = max(n - m + min(blockIdx.x * 16 + 15, rows - 1) / p.G + 1, 0);  // the most of any row
-  const CacheHead<D> c(p.cache, (int64_t)b * p.Hkv + g, p.cap);
-  typename A::Rows f;
-  A::load_rows(p, qrow, live, lg, f);
+  constexpr int LD = D + 4;  // row of the joining buffer: 16 rows start in different banks
+  __shared__ float s_o[kWaves][16 * LD];
+  __shared__ float2 s_ml[kWaves][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lg = lane >> 4, col = lane & 15;
+  const int g = blockIdx.x % p.Hkv, rb = blockIdx.x / p.Hkv % p.blocks, split = blockIdx.x / (p.Hkv * p.blocks);
+  const int b = blockIdx.y;
+  const Sample sm(p, b);
+  const int r0 = rb * 16 * MT;
+  if (r0 >= sm.rows) return;
+  const int most = sm.seen(p, min(r0 + 16 * MT, sm.rows) - 1);  // keys that the block's last row sees
+  const int begin = split * p.split_len, end = min(begin + p.split_len, most);
+  if (begin >= end && split > 0) return;
+  const int all = sm.seen(p, r0);  // keys that every row of the block sees
+  const int64_t head = (int64_t)b * p.Hkv + g;
+  const CacheHead<D> c(p.cache, head, p.cap);
 
-  f32x4 acc[A::kTiles];
+  typename A::Rows f[MT];
+  int seen[MT];
 #pragma unroll
-  for (int t = 0; t < A::kTiles; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float mx = -INFINITY, sum = 0.f;
-  for (int k0 = 0; k0 < last; k0 += 32) {
-    float x[8];
-    float top = -INFINITY;
+  for (int mt = 0; mt < MT; ++mt) {
+    const int r = r0 + 16 * mt + col;
+    const bool live = r < sm.rows;
+    seen[mt] = live ? sm.seen(p, r) : 0;
+    A::load_rows(p, live ? sm.qrow(p, g, r) : 0, live, lg, f[mt]);
+  }
+  f32x4 acc[MT][A::kTiles];
+  float ref[MT], sum[MT];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f32x4 s = A::logits(c, p.cap, k0 + 16 * h, lg, col, f);
+  for (int mt = 0; mt < MT; ++mt) {
+    ref[mt] = -INFINITY;
+    sum[mt] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[4 * h + i] = k0 + 16 * h + 4 * lg + i < seen ? s[i] * p.scale_log2 : -INFINITY;
-        top = fmaxf(top, x[4 * h + i]);
-      }
-    }
-    top = fmaxf(mx, max_xor32(max_xor16(top)));
-    // a row without a finite logit so far keeps 0 as its reference: exp2(-inf) = 0
-    const float ref = top == -INFINITY ? 0.f : top;
-    const float alpha = __builtin_amdgcn_exp2f(mx - ref);
-    mx = top;
-    sum *= alpha;
-    bf16x8 pf[TERMS];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool see = k0 + 16 * (i >> 2) + 4 * lg + (i & 3) < seen;
-      const float e = see ? __builtin_amdgcn_exp2f(x[i] - ref) : 0.f;
-      sum += e;
-      __bf16 s[TERMS];
-      split_terms<TERMS>(e, s);
-#pragma unroll
-      for (int k = 0; k < TERMS; ++k) pf[k][i] = s[k];
-    }
-#pragma unroll
-    for (int t = 0; t < A::kTiles; ++t)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[t][i] *= alpha;
+    for (int t = 0; t < A::kTiles; ++t) acc[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
-    // V: elements col*ET.. of the lane's eight keys, then keys side by side
-    bf16x8 vt[ET];
+  typename A::Key kn[2];
+  typename A::Value vn;
+  int k0 = begin + wave * kKeys;
+  if (k0 < end) {
+    A::load_key(c, p.cap, k0, lg, col, kn[0]);
+    A::load_key(c, p.cap, k0 + 16, lg, col, kn[1]);
+    A::load_value(c, p.cap, k0, lg, col, vn);
+  }
+  for (; k0 < end; k0 += kStep) {
+    bf16x8 kf[2][A::kSteps], vf[A::kTiles];
+    const bool masked = k0 + kKeys > all;  // some row does not see some key
+    const uint32_t vs0 = vn.scale[0], vs1 = vn.scale[1];
     bool nan_here = false;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      const int key = k0 + 16 * (kk >> 2) + 4 * lg + (kk & 3);
-      uint32_t byte = c.vs[(int64_t)(col * ET / kCacheBlock) * p.cap + key];
+    if (masked) {
       // rows behind the length hold anything, and a NaN block may be hidden from
       // some of the rows: both are left out here
-      nan_here |= byte == 255u && key < n;
-      if (key >= n || byte == 255u) byte = 0;
-      const uint8_t* src = c.vc + (int64_t)key * (D / 2) + col * (ET / 2);
-      const uint32_t w = ET == 8 ? *reinterpret_cast<const uint32_t*>(src) : *reinterpret_cast<const uint16_t*>(src);
-      const bf16x8 v = decode8(w, e8m0_scale(byte));
 #pragma unroll
-      for (int t = 0; t < ET; ++t) vt[t][kk] = v[t];
+      for (int kk = 0; kk < 8; ++kk) {
+        const int key = k0 + 16 * (kk >> 2) + 4 * lg + (kk & 3);
+        const uint32_t byte = ((kk < 4 ? vs0 : vs1) >> (8 * (kk & 3))) & 255u;
+        nan_here |= byte == 255u && key < sm.n;
+        if (key >= sm.n || byte == 255u) vn.scale[kk >> 2] &= ~(255u << (8 * (kk & 3)));
+      }
+    }
+    A::decode_key(kn[0], kf[0]);
+    A::decode_key(kn[1], kf[1]);
+    A::decode_value(vn, vf);
+    if (k0 + kStep < end) {
+      A::load_key(c, p.cap, k0 + kStep, lg, col, kn[0]);
+      A::load_key(c, p.cap, k0 + kStep + 16, lg, col, kn[1]);
+      A::load_value(c, p.cap, k0 + kStep, lg, col, vn);
     }
 #pragma unroll
-    for (int t = 0; t < ET; ++t)
+    for (int mt = 0; mt < MT; ++mt) {
+      float x[8];
 #pragma unroll
-      for (int k = TERMS - 1; k >= 0; --k)
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[t], pf[k], acc[t], 0, 0, 0);
-    if (__any(nan_here)) {  // NaN blocks reach the rows that see them
-      bool bad = false;
-      for (int kk = 0; kk < 32; ++kk)
-        bad |= k0 + kk < seen && c.vs[(int64_t)(lg * D / 128) * p.cap + k0 + kk] == 255u;
-      if (bad) {
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 s = A::logits(kf[h], f[mt]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * h + i] = s[i];
+      }
+      if (KEEP && r0 + 16 * mt + col < p.wrows) {
+        float* dst = p.logit + (head * p.wrows + r0 + 16 * mt + col) * p.lpad + k0 + 4 * lg;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float4*>(dst + 16 * h) =
+              make_float4(x[4 * h] * p.scale_log2, x[4 * h + 1] * p.scale_log2, x[4 * h + 2] * p.scale_log2,
+                          x[4 * h + 3] * p.scale_log2);
+      }
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (k0 + 16 * (i >> 2) + 4 * lg + (i & 3) >= seen[mt]) x[i] = -INFINITY;
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      top *= p.scale_log2;
+      if (__any(top > ref[mt] + kSlack)) {
+        top = fmaxf(ref[mt], max_xor32(max_xor16(top)));
+        // a row without a finite logit so far keeps 0 as its reference: exp2(-inf) = 0
+        const float alpha = __builtin_amdgcn_exp2f(ref[mt] - (top == -INFINITY ? 0.f : top));
+        ref[mt] = top;
+        sum[mt] *= alpha;
 #pragma unroll
         for (int t = 0; t < A::kTiles; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_nanf("");
+          for (int i = 0; i < 4; ++i) acc[mt][t][i] *= alpha;
+      }
+      const float base = ref[mt] == -INFINITY ? 0.f : ref[mt];
+      bf16x8 pf[TERMS];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float e = __builtin_amdgcn_exp2f(fmaf(x[i], p.scale_log2, -base));
+        sum[mt] += e;
+        __bf16 s[TERMS];
+        split_terms<TERMS>(e, s);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) pf[k][i] = s[k];
+      }
+#pragma unroll
+      for (int t = 0; t < A::kTiles; ++t)
+#pragma unroll
+        for (int k = TERMS - 1; k >= 0; --k)
+          acc[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[t], pf[k], acc[mt][t], 0, 0, 0);
+    }
+    if (masked && __any(nan_here)) {  // NaN blocks reach the rows that see them
+      const uint8_t* sc = c.vs + ((uint32_t)(lg * D / 128) * (uint32_t)p.cap + k0);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        bool bad = false;
+        for (int kk = 0; kk < kKeys; ++kk) bad |= k0 + kk < seen[mt] && sc[kk] == 255u;
+#pragma unroll
+        for (int t = 0; t < A::kTiles; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[mt][t][i] = bad ? __builtin_nanf("") : acc[mt][t][i];
       }
     }
   }
-  sum = sum_xor32(sum_xor16(sum));
-  if (!live) return;
-  const float inv = seen > 0 ? 1.f / sum : 0.f;  // all logits -inf: 0 * inf, a NaN
-  if (lg == 0 && qi < p.weight_rows)
-    p.stat[((int64_t)b * p.Hkv + g) * p.weight_rows * p.G + r] = make_float2(mx == -INFINITY ? 0.f : mx, inv);
+
+  // The waves' parts, 16 rows at a time.
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int mt = 0; mt < MT; ++mt) {
+    const float l = sum_xor32(sum_xor16(sum[mt]));
+    if (mt > 0) __syncthreads();
+    if (lg == 0) s_ml[wave][col] = make_float2(ref[mt], l);
 #pragma unroll
-    for (int t = 0; t < ET; ++t) {
-      const int64_t e = qrow * D + (4 * lg + i) * ET + t;
-      const float y = acc[t][i] * inv;
-      if constexpr (TERMS == 3) static_cast<float*>(p.o)[e] = y;
-      else static_cast<__bf16*>(p.o)[e] = (__bf16)y;
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < A::kTiles; t += 4)
+        *reinterpret_cast<float4*>(&s_o[wave][col * LD + (4 * lg + i) * A::kTiles + t]) =
+            make_float4(acc[mt][t][i], acc[mt][t + 1][i], acc[mt][t + 2][i], acc[mt][t + 3][i]);
+    __syncthreads();
+    constexpr int TPR = kThreads / 16, EPT = D / TPR;  // threads of a row, elements of a thread
+    const int row = tid / TPR, e0 = tid % TPR * EPT, r = r0 + 16 * mt + row;
+    if (r >= sm.rows) continue;  // the barriers are outside
+    float top = -INFINITY, w[kWaves], all_l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, s_ml[k][row].x);
+    const float base = top == -INFINITY ? 0.f : top;
+    float y[EPT];
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) y[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      w[k] = __builtin_amdgcn_exp2f(s_ml[k][row].x - base);
+      all_l = fmaf(w[k], s_ml[k][row].y, all_l);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) y[e] = fmaf(w[k], s_o[k][row * LD + e0 + e], y[e]);
+    }
+    if (p.nsplit == 1) {
+      const bool some = sm.seen(p, r) > 0;
+      const float inv = some ? 1.f / all_l : 0.f;  // every logit -inf: 0 * inf, a NaN
+      const int64_t at = sm.qrow(p, g, r) * D + e0;
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        const float z = some ? y[e] * inv : 0.f;
+        if constexpr (A::kF32) static_cast<float*>(p.o)[at + e] = z;
+        else static_cast<__bf16*>(p.o)[at + e] = (__bf16)z;
+      }
+      if (e0 == 0 && r < p.wrows) p.stat[head * p.wrows + r] = make_float2(base, inv);
+    } else {
+      const int64_t at = (head * p.rows + r) * p.nsplit + split;
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) p.part_o[at * D + e0 + e] = y[e];
+      if (e0 == 0) p.part_ml[at] = make_float2(top, all_l);
     }
   }
 }
 
-// One wave: the weight of 16 keys, the logits taken again.
+// Splits of row r that hold a key of its block (at least one: it writes the row).
+template <int MT>
+__device__ __forceinline__ int live_splits(const AttnParams& p, const Sample& sm, int r) {
+  const int r0 = r / (16 * MT) * 16 * MT;
+  const int most = sm.seen(p, min(r0 + 16 * MT, sm.rows) - 1);
+  return max((most + p.split_len - 1) / p.split_len, 1);
+}
+
+// (reference, 1 / sum) of row r over its splits.
+__device__ __forceinline__ float2 join_stat(const float2* ml, int ns, bool some) {
+  float top = -INFINITY, l = 0.f;
+  for (int s = 0; s < ns; ++s) top = fmaxf(top, ml[s].x);
+  const float base = top == -INFINITY ? 0.f : top;
+  for (int s = 0; s < ns; ++s) l = fmaf(__builtin_amdgcn_exp2f(ml[s].x - base), ml[s].y, l);
+  return make_float2(base, some ? 1.f / l : 0.f);
+}
+
+// One wave a row: joins the splits in their order.
+template <int D, int TERMS, int MT>
+__global__ __launch_bounds__(kThreads) void cache4_join_kernel(AttnParams p) {
+  constexpr int EPL = D / kWave;
+  const int g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
+  const Sample sm(p, b);
+  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (r >= sm.rows) return;
+  const int64_t head = (int64_t)b * p.Hkv + g;
+  const int ns = live_splits<MT>(p, sm, r);
+  const bool some = sm.seen(p, r) > 0;
+  const int64_t at = (head * p.rows + r) * p.nsplit;
+  const float2* ml = p.part_ml + at;
+  const float2 st = join_stat(ml, ns, some);
+  float y[EPL];
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) y[e] = 0.f;
+  for (int s = 0; s < ns; ++s) {
+    const float w = __builtin_amdgcn_exp2f(ml[s].x - st.x);
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) y[e] = fmaf(w, p.part_o[(at + s) * D + lane * EPL + e], y[e]);
+  }
+  const int64_t to = sm.qrow(p, g, r) * D + lane * EPL;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) {
+    const float z = some ? y[e] * st.y : 0.f;
+    if constexpr (TERMS == 3) static_cast<float*>(p.o)[to + e] = z;
+    else static_cast<__bf16*>(p.o)[to + e] = (__bf16)z;
+  }
+  if (lane == 0 && r < p.wrows) p.stat[head * p.wrows + r] = st;
+}
+
+// The weight of 1024 keys from the logits that the first kernel kept.
+__global__ __launch_bounds__(kThreads) void cache4_weight_kernel(AttnParams p) {
+  const int g = blockIdx.y, b = blockIdx.z;
+  const Sample sm(p, b);
+  const int k0 = (blockIdx.x * kThreads + threadIdx.x) * 4;
+  if (k0 >= sm.n) return;
+  const int64_t head = (int64_t)b * p.Hkv + g;
+  const int rows = min(sm.rows, p.wrows);
+  float w[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < rows; ++r) {
+    const int seen = sm.seen(p, r);
+    if (k0 >= seen) continue;
+    const float2 st = p.stat[head * p.wrows + r];
+    const float4 x = *reinterpret_cast<const float4*>(p.logit + (head * p.wrows + r) * p.lpad + k0);
+    const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] += k0 + i < seen ? __builtin_amdgcn_exp2f(y[i] - st.x) * st.y : 0.f;
+  }
+  const int64_t at = head * p.cap + k0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (k0 + i < sm.n) p.weight_out[at + i] = (p.weight_in ? p.weight_in[at + i] : 0.f) + w[i];
+}
+
+// The same, the logits taken again: one wave, 16 keys.
 template <int D, int TERMS>
-__global__ __launch_bounds__(64) void cache4_weight_kernel(AttnParams p) {
+__global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
   using A = Attn<D, TERMS>;
   const int b = blockIdx.z, g = blockIdx.y, lane = threadIdx.x, lg = lane >> 4, col = lane & 15;
-  const int n = min(max(p.lengths[b], 0), p.max_len);
+  const Sample sm(p, b);
   const int k0 = blockIdx.x * 16;
-  if (k0 >= n) return;
-  const int lo = p.cu[b], m = min(p.cu[b + 1] - lo, p.max_q);
-  const int rows = min(m, p.weight_rows) * p.G;
+  if (k0 >= sm.n) return;
+  const int rows = min(sm.rows, p.wrows);
   const int64_t head = (int64_t)b * p.Hkv + g;
   const CacheHead<D> c(p.cache, head, p.cap);
+  typename A::Key kn;
+  bf16x8 kf[A::kSteps];
+  A::load_key(c, p.cap, k0, lg, col, kn);
+  A::decode_key(kn, kf);
   float w[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = 0; r0 < rows; r0 += 16) {
-    const int r = r0 + col, qi = r / p.G;
+    const int r = r0 + col;
     const bool live = r < rows;
-    const int seen = live ? n - m + qi + 1 : 0;
+    const int seen = live ? sm.seen(p, r) : 0;
     typename A::Rows f;
-    A::load_rows(p, (int64_t)(lo + qi) * p.Hq + g * p.G + r % p.G, live, lg, f);
-    const float2 st = live ? p.stat[head * p.weight_rows * p.G + r] : make_float2(0.f, 0.f);
-    const f32x4 s = A::logits(c, p.cap, k0, lg, col, f);
+    A::load_rows(p, live ? sm.qrow(p, g, r) : 0, live, lg, f);
+    const float2 st = live ? p.stat[head * p.wrows + r] : make_float2(0.f, 0.f);
+    const f32x4 s = A::logits(kf, f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float e = __builtin_amdgcn_exp2f(s[i] * p.scale_log2 - st.x) * st.y;
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -st.x)) * st.y;
       w[i] += k0 + 4 * lg + i < seen ? e : 0.f;
     }
   }
@@ -243,21 +486,49 @@ __global__ __launch_bounds__(64) void cache4_weight_kernel(AttnParams p) {
   for (int i = 0; i < 4; ++i) {
     const float y = row16_sum(w[i]);
     const int key = k0 + 4 * lg + i;
-    if (col == 0 && key < n) {
+    if (col == 0 && key < sm.n) {
       const int64_t at = head * p.cap + key;
       p.weight_out[at] = (p.weight_in ? p.weight_in[at] : 0.f) + y;
     }
   }
 }
 
-template <int D, int TERMS>
-void launch(const AttnParams& p, int B, hipStream_t stream) {
-  if (p.max_q > 0)
-    hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS>), dim3(((int64_t)p.max_q * p.G + 15) / 16, p.Hkv, B), dim3(64),
-                       0, stream, p);
-  if (p.weight_rows > 0 && p.max_len > 0)
-    hipLaunchKernelGGL((cache4_weight_kernel<D, TERMS>), dim3((p.max_len + 15) / 16, p.Hkv, B), dim3(64), 0, stream,
-                       p);
+// Row tiles of a workgroup: one decoding of the keys serves up to 64 rows (32 of
+// fp32, whose operands take three times the registers).
+int row_tiles(int dtype, int64_t rows) { return rows <= 16 ? 1 : rows <= 32 || dtype == LITEVLM_F32 ? 2 : 4; }
+
+// Keeping the logits of a row costs 8 bytes a key (written and read), taking them
+// again D/2 + D/32 bytes a key for all of them.
+bool keep_logits(int wrows) { return wrows <= 8; }
+
+template <int D, int TERMS, int MT>
+void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
+  const bool weights = p.weight_rows > 0 && p.max_len > 0, keep = weights && keep_logits(p.wrows);
+  const dim3 grid(p.Hkv * p.blocks * p.nsplit, B);
+  if (keep) hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS, MT, true>), grid, dim3(kThreads), 0, stream, p);
+  else hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS, MT, false>), grid, dim3(kThreads), 0, stream, p);
+  if (p.nsplit > 1)
+    hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3((p.rows + kWaves - 1) / kWaves, p.Hkv, B),
+                       dim3(kThreads), 0, stream, p);
+  if (keep)
+    hipLaunchKernelGGL(cache4_weight_kernel, dim3((p.max_len + 4 * kThreads - 1) / (4 * kThreads), p.Hkv, B),
+                       dim3(kThreads), 0, stream, p);
+  else if (weights)
+    hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>), dim3((p.max_len + 15) / 16, p.Hkv, B), dim3(64), 0,
+                       stream, p);
+}
+
+template <int D>
+void launch_d(const AttnParams& p, int dtype, int B, hipStream_t stream) {
+  const int mt = row_tiles(dtype, p.rows);
+  if (dtype == LITEVLM_F32) {
+    if (mt == 1) launch_mt<D, 3, 1>(p, B, stream);
+    else launch_mt<D, 3, 2>(p, B, stream);
+  } else {
+    if (mt == 1) launch_mt<D, 1, 1>(p, B, stream);
+    else if (mt == 2) launch_mt<D, 1, 2>(p, B, stream);
+    else launch_mt<D, 1, 4>(p, B, stream);
+  }
 }
 
 }  // namespace
@@ -265,35 +536,64 @@ void launch(const AttnParams& p, int B, hipStream_t stream) {
 Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, int max_q, int max_len,
                                     int weight_rows) {
   Cache4AttnLayout lay;
-  lay.total = std::max<size_t>(256, (size_t)B * Hq * weight_rows * sizeof(float2));
+  const int G = Hq / Hkv;
+  const int64_t rows = (int64_t)max_q * G, wrows = (int64_t)weight_rows * G, heads = (int64_t)B * Hkv;
+  const int per = 16 * row_tiles(dtype, rows);
+  lay.blocks = (int)((rows + per - 1) / per);
+  // Splits: enough workgroups to fill the chip several times, steps of 128 keys.
+  const int64_t groups = std::max<int64_t>(heads * lay.blocks, 1);
+  const int64_t steps = std::max((max_len + kStep - 1) / kStep, 1);
+  const int64_t want = std::min<int64_t>(steps, (kGroupsWanted + groups - 1) / groups);
+  const int64_t each = (steps + want - 1) / want;
+  lay.split_len = (int)(each * kStep);
+  lay.nsplit = (int)((steps + each - 1) / each);
+  lay.lpad = (max_len + kKeys - 1) / kKeys * kKeys;
+  const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t parts = lay.nsplit > 1 ? (size_t)heads * rows * lay.nsplit : 0;
+  lay.part_o_off = 0;
+  lay.part_ml_off = up(parts * D * sizeof(float));
+  lay.stat_off = lay.part_ml_off + up(parts * sizeof(float2));
+  lay.logit_off = lay.stat_off + up((size_t)heads * wrows * sizeof(float2));
+  lay.total = lay.logit_off + (keep_logits((int)std::min<int64_t>(wrows, 1 << 20))
+                                   ? up((size_t)heads * wrows * lay.lpad * sizeof(float))
+                                   : 0);
+  lay.total = std::max<size_t>(lay.total, 256);
   return lay;
 }
 
 hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream) {
-  const AttnParams p{a.q,
-                     a.o,
-                     static_cast<const uint8_t*>(a.cache),
-                     a.cu_q,
-                     a.lengths,
-                     a.weight_in,
-                     a.weight_out,
-                     static_cast<float2*>(a.workspace),
-                     a.Hq,
-                     a.Hkv,
-                     a.Hq / a.Hkv,
-                     a.cap,
-                     a.max_q,
-                     a.max_len,
-                     a.weight_rows,
-                     a.scale_log2};
-  const bool bf16 = a.dtype == LITEVLM_BF16;
-  if (a.D == 128) {
-    if (bf16) launch<128, 1>(p, a.B, stream);
-    else launch<128, 3>(p, a.B, stream);
-  } else {
-    if (bf16) launch<64, 1>(p, a.B, stream);
-    else launch<64, 3>(p, a.B, stream);
-  }
+  if (a.max_q == 0) return hipSuccess;
+  const Cache4AttnLayout lay =
+      cache4_attn_layout(a.dtype, a.B, a.Hq, a.Hkv, a.D, a.max_q, a.max_len, a.weight_rows);
+  uint8_t* ws = static_cast<uint8_t*>(a.workspace);
+  AttnParams p;
+  p.q = a.q;
+  p.o = a.o;
+  p.cache = static_cast<const uint8_t*>(a.cache);
+  p.cu = a.cu_q;
+  p.lengths = a.lengths;
+  p.weight_in = a.weight_in;
+  p.weight_out = a.weight_out;
+  p.part_o = reinterpret_cast<float*>(ws + lay.part_o_off);
+  p.part_ml = reinterpret_cast<float2*>(ws + lay.part_ml_off);
+  p.stat = reinterpret_cast<float2*>(ws + lay.stat_off);
+  p.logit = reinterpret_cast<float*>(ws + lay.logit_off);
+  p.Hq = a.Hq;
+  p.Hkv = a.Hkv;
+  p.G = a.Hq / a.Hkv;
+  p.cap = a.cap;
+  p.max_q = a.max_q;
+  p.max_len = a.max_len;
+  p.weight_rows = a.weight_rows;
+  p.rows = a.max_q * p.G;
+  p.wrows = a.weight_rows * p.G;
+  p.blocks = lay.blocks;
+  p.nsplit = lay.nsplit;
+  p.split_len = lay.split_len;
+  p.lpad = lay.lpad;
+  p.scale_log2 = a.scale_log2;
+  if (a.D == 128) launch_d<128>(p, a.dtype, a.B, stream);
+  else launch_d<64>(p, a.dtype, a.B, stream);
   return hipGetLastError();
 }
 

@@ -147,9 +147,15 @@ struct Cache4RowsArgs {
 hipError_t launch_cache4_append(const Cache4RowsArgs& a, hipStream_t stream);
 hipError_t launch_cache4_read(const Cache4RowsArgs& a, hipStream_t stream);
 
-// Workspace of the attention over the 4-bit cache.
+// Workspace of the attention over the 4-bit cache, and how the rows of a KV head
+// (the queries of its heads) and the keys are dealt to workgroups:
+//   part_o   float  [B][Hkv][rows][nsplit][D]  unnormalised outputs of the key splits
+//   part_ml  float2 [B][Hkv][rows][nsplit]     their (reference, sum)
+//   stat     float2 [B][Hkv][weight rows]      (reference, 1 / sum) of the rows that add weight
+//   logit    float  [B][Hkv][weight rows][lpad] their logits, where they are kept
 struct Cache4AttnLayout {
-  size_t total;
+  int blocks, nsplit, split_len, lpad;
+  size_t part_o_off, part_ml_off, stat_off, logit_off, total;
 };
 Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, int max_q, int max_len,
                                     int weight_rows);
