@@ -39,4 +39,12 @@ __device__ __forceinline__ bf16x8 decode8(uint32_t w, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The two codes of byte j (a constant after unrolling) of w, as packed bf16.
+__device__ __forceinline__ uint32_t decode2(uint32_t w, float scale, int j) {
+  return __builtin_bit_cast(uint32_t, j == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
+                                      : j == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
+                                      : j == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
+                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+}
+
 }  // namespace litevlm

@@ -27,7 +27,8 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kKeys = 32;              // keys of a wave's step
 constexpr int kStep = kWaves * kKeys;  // keys of a workgroup's step
-constexpr int64_t kGroupsWanted = 2048;  // workgroups of the first kernel, where the keys allow
+constexpr int kKept = 8;               // rows of a KV head whose logits are kept
+constexpr int64_t kGroupsWanted = 512;  // workgroups of the first kernel, where the keys allow
 constexpr float kSlack = 8.f;          // the running reference may lag the maximum by this (log2)
 
 struct AttnParams {
@@ -131,18 +132,20 @@ struct Attn {
     }
     k.scale = c.ks[(uint32_t)(lg * D / 128) * (uint32_t)cap + k0 + col];
   }
-  // Logits (without the scale) of 16 rows against those keys.
-  static __device__ __forceinline__ f32x4 logits(const bf16x8* k, const Rows& f) {
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  // Logits (without the scale) of 16 * MT rows against those keys.
+  template <int MT>
+  static __device__ __forceinline__ void logits(const Key& k, const Rows* f, f32x4* s) {
 #pragma unroll
-    for (int t = 0; t < kSteps; ++t)
+    for (int mt = 0; mt < MT; ++mt) s[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int n = TERMS - 1; n >= 0; --n) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t], f.q[t][n], s, 0, 0, 0);
-    return s;
-  }
-  static __device__ __forceinline__ void decode_key(const Key& k, bf16x8* out) {
+    for (int t = 0; t < kSteps; ++t) {
+      const bf16x8 x = decode8(k.w[t], e8m0_scale(k.scale));
 #pragma unroll
-    for (int t = 0; t < kSteps; ++t) out[t] = decode8(k.w[t], e8m0_scale(k.scale));
+      for (int n = TERMS - 1; n >= 0; --n)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[mt].q[t][n], s[mt], 0, 0, 0);
+    }
   }
 
   // The lane's share of 32 values: elements col*D/16.. of keys 16h + 4lg + i, and
@@ -162,27 +165,37 @@ struct Attn {
     v.scale[0] = *reinterpret_cast<const uint32_t*>(sc);
     v.scale[1] = *reinterpret_cast<const uint32_t*>(sc + 16);
   }
-  // Element t of the lane's eight keys, for every t: pairs of elements of a key
-  // become pairs of keys of an element.
-  static __device__ __forceinline__ void decode_value(const Value& v, bf16x8* out) {
-    uint32_t d[8][kTiles / 2];
+  // O^T += V^T P^T. Two elements of a key come from one byte; pairs of elements of
+  // a key become pairs of keys of an element.
+  template <int MT>
+  static __device__ __forceinline__ void add_values(const Value& v, const bf16x8 (*pf)[TERMS], f32x4 (*acc)[kTiles]) {
+    float scale[8];
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
-      const uint32_t byte = (v.scale[kk >> 2] >> (8 * (kk & 3))) & 255u;
-      const i32x4 x = __builtin_bit_cast(i32x4, decode8(v.w[kk], e8m0_scale(byte)));
-#pragma unroll
-      for (int t = 0; t < kTiles / 2; ++t) d[kk][t] = (uint32_t)x[t];
+      const uint32_t w = v.scale[kk >> 2];
+      const int by = 23 - 8 * (kk & 3);  // the key's byte to the exponent's place
+      scale[kk] = __uint_as_float((by >= 0 ? w << by : w >> -by) & 0x7F800000u);
     }
 #pragma unroll
-    for (int t = 0; t < kTiles / 2; ++t) {
+    for (int j = 0; j < kTiles / 2; ++j) {
+      uint32_t d[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) d[kk] = decode2(v.w[kk], scale[kk], j);
       i32x4 even, odd;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        even[j] = (int)__builtin_amdgcn_perm(d[2 * j + 1][t], d[2 * j][t], 0x05040100u);
-        odd[j] = (int)__builtin_amdgcn_perm(d[2 * j + 1][t], d[2 * j][t], 0x07060302u);
+      for (int i = 0; i < 4; ++i) {
+        even[i] = (int)__builtin_amdgcn_perm(d[2 * i + 1], d[2 * i], 0x05040100u);
+        odd[i] = (int)__builtin_amdgcn_perm(d[2 * i + 1], d[2 * i], 0x07060302u);
       }
-      out[2 * t] = __builtin_bit_cast(bf16x8, even);
-      out[2 * t + 1] = __builtin_bit_cast(bf16x8, odd);
+#pragma unroll
+      for (int k = TERMS - 1; k >= 0; --k)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          acc[mt][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), pf[mt][k],
+                                                                   acc[mt][2 * j], 0, 0, 0);
+          acc[mt][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), pf[mt][k],
+                                                                       acc[mt][2 * j + 1], 0, 0, 0);
+        }
     }
   }
 };
@@ -194,12 +207,13 @@ struct Attn {
 // probabilities are at most 2^kSlack, and neither an exchange between lanes nor a
 // rescaling of the output is needed.
 template <int D, int TERMS, int MT, bool KEEP>
-__global__ __launch_bounds__(kThreads) void cache4_attn_kernel(AttnParams p) {
+__global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache4_attn_kernel(AttnParams p) {
   using A = Attn<D, TERMS>;
   constexpr int LD = D + 4;  // row of the joining buffer: 16 rows start in different banks
   __shared__ float s_o[kWaves][16 * LD];
   __shared__ float2 s_ml[kWaves][16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lg = lane >> 4, col = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, lg = lane >> 4, col = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = blockIdx.x % p.Hkv, rb = blockIdx.x / p.Hkv % p.blocks, split = blockIdx.x / (p.Hkv * p.blocks);
   const int b = blockIdx.y;
   const Sample sm(p, b);
@@ -231,6 +245,7 @@ __global__ __launch_bounds__(kThreads) void cache4_attn_kernel(AttnParams p) {
     for (int t = 0; t < A::kTiles; ++t) acc[mt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  uint32_t bad = 0;  // row tiles whose lane's outputs are NaN
   typename A::Key kn[2];
   typename A::Value vn;
   int k0 = begin + wave * kKeys;
@@ -240,51 +255,56 @@ __global__ __launch_bounds__(kThreads) void cache4_attn_kernel(AttnParams p) {
     A::load_value(c, p.cap, k0, lg, col, vn);
   }
   for (; k0 < end; k0 += kStep) {
-    bf16x8 kf[2][A::kSteps], vf[A::kTiles];
-    const bool masked = k0 + kKeys > all;  // some row does not see some key
-    const uint32_t vs0 = vn.scale[0], vs1 = vn.scale[1];
-    bool nan_here = false;
-    if (masked) {
-      // rows behind the length hold anything, and a NaN block may be hidden from
-      // some of the rows: both are left out here
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        const int key = k0 + 16 * (kk >> 2) + 4 * lg + (kk & 3);
-        const uint32_t byte = ((kk < 4 ? vs0 : vs1) >> (8 * (kk & 3))) & 255u;
-        nan_here |= byte == 255u && key < sm.n;
-        if (key >= sm.n || byte == 255u) vn.scale[kk >> 2] &= ~(255u << (8 * (kk & 3)));
-      }
-    }
-    A::decode_key(kn[0], kf[0]);
-    A::decode_key(kn[1], kf[1]);
-    A::decode_value(vn, vf);
+    const typename A::Key kc[2] = {kn[0], kn[1]};
+    typename A::Value vc = vn;
     if (k0 + kStep < end) {
       A::load_key(c, p.cap, k0 + kStep, lg, col, kn[0]);
       A::load_key(c, p.cap, k0 + kStep + 16, lg, col, kn[1]);
       A::load_value(c, p.cap, k0 + kStep, lg, col, vn);
     }
+    f32x4 s[2][MT];
+    A::template logits<MT>(kc[0], f, s[0]);
+    A::template logits<MT>(kc[1], f, s[1]);
+    if (KEEP) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        if (r0 + 16 * mt + col >= p.wrows) continue;
+        float* dst = p.logit + (head * p.wrows + r0 + 16 * mt + col) * p.lpad + k0 + 4 * lg;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(dst + 16 * h) = s[h][mt] * p.scale_log2;
+      }
+    }
+    if (k0 + kKeys > all) {  // some row does not see some key
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (k0 + 16 * (i >> 2) + 4 * lg + (i & 3) >= seen[mt]) s[i >> 2][mt][i & 3] = -INFINITY;
+      // rows behind the length hold anything, and a NaN block may be hidden from
+      // some of the rows: both are left out of the product
+      bool nan_here = false;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        const int key = k0 + 16 * (kk >> 2) + 4 * lg + (kk & 3);
+        const uint32_t ones = 255u << (8 * (kk & 3));
+        const bool nan = (vc.scale[kk >> 2] & ones) == ones;
+        nan_here |= nan && key < sm.n;
+        if (nan || key >= sm.n) vc.scale[kk >> 2] &= ~ones;
+      }
+      if (__any(nan_here)) {  // but reach the rows that see them
+        const uint8_t* sc = c.vs + ((uint32_t)(lg * D / 128) * (uint32_t)p.cap + k0);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          for (int kk = 0; kk < kKeys; ++kk)
+            if (k0 + kk < seen[mt] && sc[kk] == 255u) bad |= 1u << mt;
+      }
+    }
+    bf16x8 pf[MT][TERMS];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       float x[8];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 s = A::logits(kf[h], f[mt]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * h + i] = s[i];
-      }
-      if (KEEP && r0 + 16 * mt + col < p.wrows) {
-        float* dst = p.logit + (head * p.wrows + r0 + 16 * mt + col) * p.lpad + k0 + 4 * lg;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<float4*>(dst + 16 * h) =
-              make_float4(x[4 * h] * p.scale_log2, x[4 * h + 1] * p.scale_log2, x[4 * h + 2] * p.scale_log2,
-                          x[4 * h + 3] * p.scale_log2);
-      }
-      if (masked) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (k0 + 16 * (i >> 2) + 4 * lg + (i & 3) >= seen[mt]) x[i] = -INFINITY;
-      }
+      for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][mt][i & 3];
       float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
       top *= p.scale_log2;
       if (__any(top > ref[mt] + kSlack)) {
@@ -299,35 +319,24 @@ __global__ __launch_bounds__(kThreads) void cache4_attn_kernel(AttnParams p) {
           for (int i = 0; i < 4; ++i) acc[mt][t][i] *= alpha;
       }
       const float base = ref[mt] == -INFINITY ? 0.f : ref[mt];
-      bf16x8 pf[TERMS];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        float e = __builtin_amdgcn_exp2f(fmaf(x[i], p.scale_log2, -base));
+        const float e = __builtin_amdgcn_exp2f(fmaf(x[i], p.scale_log2, -base));
         sum[mt] += e;
-        __bf16 s[TERMS];
-        split_terms<TERMS>(e, s);
+        __bf16 z[TERMS];
+        split_terms<TERMS>(e, z);
 #pragma unroll
-        for (int k = 0; k < TERMS; ++k) pf[k][i] = s[k];
-      }
-#pragma unroll
-      for (int t = 0; t < A::kTiles; ++t)
-#pragma unroll
-        for (int k = TERMS - 1; k >= 0; --k)
-          acc[mt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[t], pf[k], acc[mt][t], 0, 0, 0);
-    }
-    if (masked && __any(nan_here)) {  // NaN blocks reach the rows that see them
-      const uint8_t* sc = c.vs + ((uint32_t)(lg * D / 128) * (uint32_t)p.cap + k0);
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        bool bad = false;
-        for (int kk = 0; kk < kKeys; ++kk) bad |= k0 + kk < seen[mt] && sc[kk] == 255u;
-#pragma unroll
-        for (int t = 0; t < A::kTiles; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[mt][t][i] = bad ? __builtin_nanf("") : acc[mt][t][i];
+        for (int k = 0; k < TERMS; ++k) pf[mt][k][i] = z[k];
       }
     }
+    A::template add_values<MT>(vc, pf, acc);
   }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int t = 0; t < A::kTiles; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[mt][t][i] = bad >> mt & 1 ? __builtin_nanf("") : acc[mt][t][i];
 
   // The waves' parts, 16 rows at a time.
 #pragma unroll
@@ -369,7 +378,10 @@ __global__ __launch_bounds__(kThreads) void cache4_attn_kernel(AttnParams p) {
         if constexpr (A::kF32) static_cast<float*>(p.o)[at + e] = z;
         else static_cast<__bf16*>(p.o)[at + e] = (__bf16)z;
       }
-      if (e0 == 0 && r < p.wrows) p.stat[head * p.wrows + r] = make_float2(base, inv);
+      if (e0 == 0 && r < p.wrows) {
+        if (KEEP) p.part_ml[head * p.rows + r] = make_float2(top, all_l);
+        else p.stat[head * p.wrows + r] = make_float2(base, inv);
+      }
     } else {
       const int64_t at = (head * p.rows + r) * p.nsplit + split;
 #pragma unroll
@@ -387,69 +399,120 @@ __device__ __forceinline__ int live_splits(const AttnParams& p, const Sample& sm
   return max((most + p.split_len - 1) / p.split_len, 1);
 }
 
-// (reference, 1 / sum) of row r over its splits.
+// (reference, 1 / sum) of a row over its ns splits, by one wave; the same in every lane.
 __device__ __forceinline__ float2 join_stat(const float2* ml, int ns, bool some) {
-  float top = -INFINITY, l = 0.f;
-  for (int s = 0; s < ns; ++s) top = fmaxf(top, ml[s].x);
+  const int lane = threadIdx.x & 63;
+  float2 x = lane < ns ? ml[lane] : make_float2(-INFINITY, 0.f);
+  float top = x.x;
+  for (int s = lane + kWave; s < ns; s += kWave) top = fmaxf(top, ml[s].x);
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) top = wave_max_xor(top, k);
   const float base = top == -INFINITY ? 0.f : top;
-  for (int s = 0; s < ns; ++s) l = fmaf(__builtin_amdgcn_exp2f(ml[s].x - base), ml[s].y, l);
+  float l = __builtin_amdgcn_exp2f(x.x - base) * x.y;
+  for (int s = lane + kWave; s < ns; s += kWave) l = fmaf(__builtin_amdgcn_exp2f(ml[s].x - base), ml[s].y, l);
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) l += __shfl_xor(l, k, kWave);
   return make_float2(base, some ? 1.f / l : 0.f);
 }
 
-// One wave a row: joins the splits in their order.
+// Two kinds of workgroup. The first p.rows of a KV head (where the keys were
+// split) join one row's splits: thread (slot, piece) sums 16 bytes of splits slot,
+// slot + SLOTS, ..., the slots are then summed in order. The others (where the
+// logits were kept) take the weight of 1024 keys each.
 template <int D, int TERMS, int MT>
-__global__ __launch_bounds__(kThreads) void cache4_join_kernel(AttnParams p) {
-  constexpr int EPL = D / kWave;
-  const int g = blockIdx.y, b = blockIdx.z, lane = threadIdx.x & 63;
+__global__ __launch_bounds__(kThreads) void cache4_join_kernel(AttnParams p, int joins) {
+  constexpr int V4 = D / 4, SLOTS = kThreads / V4;
+  const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const Sample sm(p, b);
-  const int r = blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (r >= sm.rows) return;
   const int64_t head = (int64_t)b * p.Hkv + g;
-  const int ns = live_splits<MT>(p, sm, r);
-  const bool some = sm.seen(p, r) > 0;
-  const int64_t at = (head * p.rows + r) * p.nsplit;
-  const float2* ml = p.part_ml + at;
-  const float2 st = join_stat(ml, ns, some);
-  float y[EPL];
+  if ((int)blockIdx.x < joins) {
+    __shared__ float4 s_part[SLOTS][V4];
+    const int r = blockIdx.x;
+    if (r >= sm.rows) return;
+    const int ns = live_splits<MT>(p, sm, r);
+    const bool some = sm.seen(p, r) > 0;
+    const int64_t at = (head * p.rows + r) * p.nsplit;
+    const float2* ml = p.part_ml + at;
+    const float4* po = reinterpret_cast<const float4*>(p.part_o + at * D);
+    const int slot = tid / V4, c = tid % V4;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    // the first of the thread's splits are requested before the sum is known
+    constexpr int R = 4;
+    float4 x[R];
+    float m[R];
 #pragma unroll
-  for (int e = 0; e < EPL; ++e) y[e] = 0.f;
-  for (int s = 0; s < ns; ++s) {
-    const float w = __builtin_amdgcn_exp2f(ml[s].x - st.x);
+    for (int i = 0; i < R; ++i) {
+      const int s = min(slot + i * SLOTS, ns - 1);
+      x[i] = po[s * V4 + c];
+      m[i] = ml[s].x;
+    }
+    const float2 st = join_stat(ml, ns, some);
+    const auto add = [&](float w, const float4& z) __attribute__((always_inline)) {
+      y.x = fmaf(w, z.x, y.x), y.y = fmaf(w, z.y, y.y), y.z = fmaf(w, z.z, y.z), y.w = fmaf(w, z.w, y.w);
+    };
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) y[e] = fmaf(w, p.part_o[(at + s) * D + lane * EPL + e], y[e]);
+    for (int i = 0; i < R; ++i)
+      if (slot + i * SLOTS < ns) add(__builtin_amdgcn_exp2f(m[i] - st.x), x[i]);
+#pragma unroll 4
+    for (int s = slot + R * SLOTS; s < ns; s += SLOTS) add(__builtin_amdgcn_exp2f(ml[s].x - st.x), po[(int64_t)s * V4 + c]);
+    s_part[slot][c] = y;
+    __syncthreads();
+    if (tid < V4) {
+      float4 t = s_part[0][tid];
+#pragma unroll
+      for (int k = 1; k < SLOTS; ++k) {
+        const float4 u = s_part[k][tid];
+        t.x += u.x, t.y += u.y, t.z += u.z, t.w += u.w;
+      }
+      const float z[4] = {t.x, t.y, t.z, t.w};
+      const int64_t to = sm.qrow(p, g, r) * D + tid * 4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = some ? z[e] * st.y : 0.f;
+        if constexpr (TERMS == 3) static_cast<float*>(p.o)[to + e] = v;
+        else static_cast<__bf16*>(p.o)[to + e] = (__bf16)v;
+      }
+      if (tid == 0 && r < p.wrows) p.stat[head * p.wrows + r] = st;
+    }
+    return;
   }
-  const int64_t to = sm.qrow(p, g, r) * D + lane * EPL;
-#pragma unroll
-  for (int e = 0; e < EPL; ++e) {
-    const float z = some ? y[e] * st.y : 0.f;
-    if constexpr (TERMS == 3) static_cast<float*>(p.o)[to + e] = z;
-    else static_cast<__bf16*>(p.o)[to + e] = (__bf16)z;
-  }
-  if (lane == 0 && r < p.wrows) p.stat[head * p.wrows + r] = st;
-}
-
-// The weight of 1024 keys from the logits that the first kernel kept.
-__global__ __launch_bounds__(kThreads) void cache4_weight_kernel(AttnParams p) {
-  const int g = blockIdx.y, b = blockIdx.z;
-  const Sample sm(p, b);
-  const int k0 = (blockIdx.x * kThreads + threadIdx.x) * 4;
-  if (k0 >= sm.n) return;
-  const int64_t head = (int64_t)b * p.Hkv + g;
+  __shared__ float2 s_stat[kKept];
   const int rows = min(sm.rows, p.wrows);
-  float w[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int r = 0; r < rows; ++r) {
-    const int seen = sm.seen(p, r);
-    if (k0 >= seen) continue;
-    const float2 st = p.stat[head * p.wrows + r];
-    const float4 x = *reinterpret_cast<const float4*>(p.logit + (head * p.wrows + r) * p.lpad + k0);
-    const float y[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] += k0 + i < seen ? __builtin_amdgcn_exp2f(y[i] - st.x) * st.y : 0.f;
+  if (((int)blockIdx.x - joins) * kThreads * 4 >= sm.n) return;
+  for (int r = tid >> 6; r < rows; r += kWaves) {
+    const float2 st = join_stat(p.part_ml + (head * p.rows + r) * p.nsplit, live_splits<MT>(p, sm, r), sm.seen(p, r) > 0);
+    if ((tid & 63) == 0) s_stat[r] = st;
   }
+  const int k0 = (((int)blockIdx.x - joins) * kThreads + tid) * 4;
   const int64_t at = head * p.cap + k0;
+  const bool live = k0 < sm.n;
+  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 w = zero, x[kKept];
+  if (live) {
+    // rows that do not see the keys may not have written them: their numbers are not used
+    #pragma unroll
+    for (int r = 0; r < kKept; ++r)
+      x[r] = r < rows ? *reinterpret_cast<const float4*>(p.logit + (head * p.wrows + r) * p.lpad + k0) : zero;
+    if (p.weight_in) {
+      // cap is a multiple of 4 and the rows end inside it; the address may be any float's
+      w = make_float4(p.weight_in[at], p.weight_in[at + 1], p.weight_in[at + 2], p.weight_in[at + 3]);
+    }
+  }
+  __syncthreads();
+  if (!live) return;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int r = 0; r < kKept; ++r) {
+    const int seen = r < rows ? sm.seen(p, r) : 0;
+    const float2 st = s_stat[r];
+    const float y[4] = {x[r].x, x[r].y, x[r].z, x[r].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += k0 + i < seen ? __builtin_amdgcn_exp2f(y[i] - st.x) * st.y : 0.f;
+  }
+  const float v[4] = {w.x + s[0], w.y + s[1], w.z + s[2], w.w + s[3]};
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (k0 + i < sm.n) p.weight_out[at + i] = (p.weight_in ? p.weight_in[at + i] : 0.f) + w[i];
+    if (k0 + i < sm.n) p.weight_out[at + i] = v[i];
 }
 
 // The same, the logits taken again: one wave, 16 keys.
@@ -464,9 +527,7 @@ __global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
   const int64_t head = (int64_t)b * p.Hkv + g;
   const CacheHead<D> c(p.cache, head, p.cap);
   typename A::Key kn;
-  bf16x8 kf[A::kSteps];
   A::load_key(c, p.cap, k0, lg, col, kn);
-  A::decode_key(kn, kf);
   float w[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = 0; r0 < rows; r0 += 16) {
     const int r = r0 + col;
@@ -475,7 +536,8 @@ __global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
     typename A::Rows f;
     A::load_rows(p, live ? sm.qrow(p, g, r) : 0, live, lg, f);
     const float2 st = live ? p.stat[head * p.wrows + r] : make_float2(0.f, 0.f);
-    const f32x4 s = A::logits(kf, f);
+    f32x4 s;
+    A::template logits<1>(kn, &f, &s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float e = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -st.x)) * st.y;
@@ -493,13 +555,14 @@ __global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
   }
 }
 
-// Row tiles of a workgroup: one decoding of the keys serves up to 64 rows (32 of
-// fp32, whose operands take three times the registers).
-int row_tiles(int dtype, int64_t rows) { return rows <= 16 ? 1 : rows <= 32 || dtype == LITEVLM_F32 ? 2 : 4; }
+// Row tiles of a workgroup. Two decode a key once for 32 rows; four would hold 128
+// registers of outputs and leave one wave a SIMD (256 queries of 4 heads over 6528
+// rows: 2 tiles 47 us, 4 tiles 61 us, 1 tile 57 us).
+int row_tiles(int64_t rows) { return rows <= 16 ? 1 : 2; }
 
 // Keeping the logits of a row costs 8 bytes a key (written and read), taking them
 // again D/2 + D/32 bytes a key for all of them.
-bool keep_logits(int wrows) { return wrows <= 8; }
+bool keep_logits(int wrows) { return wrows <= kKept; }
 
 template <int D, int TERMS, int MT>
 void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
@@ -507,27 +570,24 @@ void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
   const dim3 grid(p.Hkv * p.blocks * p.nsplit, B);
   if (keep) hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS, MT, true>), grid, dim3(kThreads), 0, stream, p);
   else hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS, MT, false>), grid, dim3(kThreads), 0, stream, p);
-  if (p.nsplit > 1)
-    hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3((p.rows + kWaves - 1) / kWaves, p.Hkv, B),
-                       dim3(kThreads), 0, stream, p);
-  if (keep)
-    hipLaunchKernelGGL(cache4_weight_kernel, dim3((p.max_len + 4 * kThreads - 1) / (4 * kThreads), p.Hkv, B),
-                       dim3(kThreads), 0, stream, p);
-  else if (weights)
+  const int joins = p.nsplit > 1 ? p.rows : 0, chunks = keep ? (p.max_len + 4 * kThreads - 1) / (4 * kThreads) : 0;
+  if (joins + chunks > 0)
+    hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3(joins + chunks, p.Hkv, B), dim3(kThreads), 0, stream, p,
+                       joins);
+  if (weights && !keep)
     hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>), dim3((p.max_len + 15) / 16, p.Hkv, B), dim3(64), 0,
                        stream, p);
 }
 
 template <int D>
 void launch_d(const AttnParams& p, int dtype, int B, hipStream_t stream) {
-  const int mt = row_tiles(dtype, p.rows);
+  const int mt = row_tiles(p.rows);
   if (dtype == LITEVLM_F32) {
     if (mt == 1) launch_mt<D, 3, 1>(p, B, stream);
     else launch_mt<D, 3, 2>(p, B, stream);
   } else {
     if (mt == 1) launch_mt<D, 1, 1>(p, B, stream);
-    else if (mt == 2) launch_mt<D, 1, 2>(p, B, stream);
-    else launch_mt<D, 1, 4>(p, B, stream);
+    else launch_mt<D, 1, 2>(p, B, stream);
   }
 }
 
@@ -538,25 +598,31 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   Cache4AttnLayout lay;
   const int G = Hq / Hkv;
   const int64_t rows = (int64_t)max_q * G, wrows = (int64_t)weight_rows * G, heads = (int64_t)B * Hkv;
-  const int per = 16 * row_tiles(dtype, rows);
+  const int per = 16 * row_tiles(rows);
   lay.blocks = (int)((rows + per - 1) / per);
-  // Splits: enough workgroups to fill the chip several times, steps of 128 keys.
+  // Splits of whole steps of 128 keys: two workgroups a CU where there are keys for
+  // them (a ragged batch of 8 x 3200 rows, 5 queries: 512 workgroups 14.4 us, 1024
+  // 15.8 us, 1664 19.5 us: a short split's start and end cost more than its keys).
+  // With one row tile memory is the bound, and splits of 512 keys let the CUs finish
+  // together (32 samples of 10-16K rows: 512 keys 101 us, 1024 106 us, 2048 112 us,
+  // 4096 117 us).
   const int64_t groups = std::max<int64_t>(heads * lay.blocks, 1);
   const int64_t steps = std::max((max_len + kStep - 1) / kStep, 1);
-  const int64_t want = std::min<int64_t>(steps, (kGroupsWanted + groups - 1) / groups);
+  int64_t want = (kGroupsWanted + groups - 1) / groups;
+  if (per == 16) want = std::max(want, (steps + 3) / 4);
+  want = std::min(want, steps);
   const int64_t each = (steps + want - 1) / want;
   lay.split_len = (int)(each * kStep);
   lay.nsplit = (int)((steps + each - 1) / each);
   lay.lpad = (max_len + kKeys - 1) / kKeys * kKeys;
   const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  const size_t parts = lay.nsplit > 1 ? (size_t)heads * rows * lay.nsplit : 0;
+  const bool keep = keep_logits((int)wrows);
+  const size_t parts = (size_t)heads * rows * lay.nsplit;
   lay.part_o_off = 0;
-  lay.part_ml_off = up(parts * D * sizeof(float));
-  lay.stat_off = lay.part_ml_off + up(parts * sizeof(float2));
+  lay.part_ml_off = up(lay.nsplit > 1 ? parts * D * sizeof(float) : 0);
+  lay.stat_off = lay.part_ml_off + up(lay.nsplit > 1 || keep ? parts * sizeof(float2) : 0);
   lay.logit_off = lay.stat_off + up((size_t)heads * wrows * sizeof(float2));
-  lay.total = lay.logit_off + (keep_logits((int)std::min<int64_t>(wrows, 1 << 20))
-                                   ? up((size_t)heads * wrows * lay.lpad * sizeof(float))
-                                   : 0);
+  lay.total = lay.logit_off + up(keep ? (size_t)heads * wrows * lay.lpad * sizeof(float) : 0);
   lay.total = std::max<size_t>(lay.total, 256);
   return lay;
 }
