@@ -187,10 +187,10 @@ struct Cache4EvictArgs {
 hipError_t launch_cache4_evict(const Cache4EvictArgs& a, hipStream_t stream);
 
 // Workspace of the draft verification: per (sample, chunk of the vocabulary) two
-// sums in 64 bits.
+// sums in 64 bits, and per sample the accepted drafts.
 struct VerifyLayout {
   int chunks;
-  size_t total;
+  size_t acc_off, total;
 };
 VerifyLayout verify_layout(int B, int V);
 
