@@ -2,9 +2,11 @@
 // ones of largest accumulated attention weight, moved in order to a new cache.
 //
 // The weights are ranked by a 32-bit key that orders them as the reals do (NaN
-// above all, -0 with +0). The smallest key kept is found byte by byte from the
-// top (a histogram of the keys that share the bytes found so far); the rows above
-// it, and the lowest positions of those equal to it, are then numbered in order.
+// above all, -0 with +0). One workgroup a head finds the smallest key kept, 11, 11
+// and 10 bits at a time: a histogram of the keys that share the bits found so far,
+// summed from the top. The rows above it, and the lowest positions of those equal
+// to it, are then numbered in order. Each thread holds consecutive keys, so an
+// order over threads is one over positions.
 #include "cache4.hpp"
 #include "launch.hpp"
 
@@ -12,6 +14,7 @@ namespace litevlm {
 namespace {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / kWave;
+constexpr int kBins = 2048;  // two a thread
 constexpr int kMoveThreads = 256, kMoveRows = 64;
 
 struct EvictParams {
@@ -31,8 +34,40 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_add(uint32_t x) {
+  return x + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false);
+}
+
+// Exclusive sum of x over the workgroup's threads in order; s_wave is free again
+// after the next barrier.
+__device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t* s_wave, uint32_t& all) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t y = x;
+  y = dpp_add<0x111, 0xF>(y);  // row_shr 1, 2, 4, 8
+  y = dpp_add<0x112, 0xF>(y);
+  y = dpp_add<0x114, 0xF>(y);
+  y = dpp_add<0x118, 0xF>(y);
+  y = dpp_add<0x142, 0xA>(y);  // row_bcast 15, 31
+  y = dpp_add<0x143, 0xC>(y);
+  if (lane == kWave - 1) s_wave[w] = y;
+  __syncthreads();
+  uint32_t before = 0;
+  all = 0;
+#pragma unroll
+  for (int k = 0; k < kSelWaves; ++k) {
+    const uint32_t z = s_wave[k];
+    before += k < w ? z : 0u;
+    all += z;
+  }
+  return before + y - x;
+}
+
+// KPT keys a thread and tile; one tile stays in registers.
+template <int KPT>
 __global__ __launch_bounds__(kSelThreads) void cache4_select_kernel(EvictParams p) {
-  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  constexpr int kTileKeys = kSelThreads * KPT;
+  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x;
   const int n = min(max(p.lengths[b], 0), p.max_len);
   const int64_t head = (int64_t)b * p.Hkv + g;
   int32_t* kept = p.kept + head * p.budget;
@@ -46,56 +81,92 @@ __global__ __launch_bounds__(kSelThreads) void cache4_select_kernel(EvictParams 
   for (int i = tid; i < p.recent; i += kSelThreads) kept[want + i] = old + i;
   if (want == 0) return;
 
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t s_prefix, s_left;
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t s_digit, s_left;
   __shared__ uint32_t s_wave[2][kSelWaves];
-  uint32_t prefix = 0, left = want;  // keys with the prefix: `left` of the largest are wanted
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+  const int tiles = (old + kTileKeys - 1) / kTileKeys;
+  uint32_t key[KPT];
+  const auto load = [&](int tile) __attribute__((always_inline)) {
+    const int i0 = tile * kTileKeys + tid * KPT;
+    float x[KPT];
+    if (i0 + KPT <= old && (reinterpret_cast<uintptr_t>(wt) & 15) == 0) {
+#pragma unroll
+      for (int j = 0; j < KPT; j += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(wt + i0 + j);
+        x[j] = v.x, x[j + 1] = v.y, x[j + 2] = v.z, x[j + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < KPT; ++j) x[j] = i0 + j < old ? wt[i0 + j] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) key[j] = order_key(x[j]);
+  };
+
+  uint32_t prefix = 0, left = want;  // of the keys with these bits, `left` of the largest are wanted
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+    hist[tid] = 0;
+    hist[tid + kSelThreads] = 0;
     __syncthreads();
-    for (int i = tid; i < old; i += kSelThreads) {
-      const uint32_t k = order_key(wt[i]);
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
+    for (int tile = 0; tile < tiles; ++tile) {
+      if (pass == 0 || tiles > 1) load(tile);
+      const int i0 = tile * kTileKeys + tid * KPT;
+#pragma unroll
+      for (int j = 0; j < KPT; ++j) {
+        const bool in = i0 + j < old && (pass == 0 || key[j] >> (shift + bits) == prefix >> (shift + bits));
+        const uint32_t d = (key[j] >> shift) & ((1u << bits) - 1);
+        // a wave whose keys fall into one bin (zeros of rows never looked at) adds
+        // them at once: additions to one address take their turns
+        const uint64_t mask = __ballot(in);
+        if (mask == 0) continue;
+        const uint32_t lead = (uint32_t)__builtin_amdgcn_readlane((int)d, __ffsll((unsigned long long)mask) - 1);
+        if (__ballot(in && d != lead) == 0) {
+          if ((tid & 63) == 0) atomicAdd(&hist[lead], (uint32_t)__popcll(mask));
+        } else if (in) {
+          atomicAdd(&hist[d], 1u);
+        }
+      }
     }
     __syncthreads();
-    if (tid == 0) {
-      uint32_t seen = 0;
-      int d = 255;
-      while (seen + hist[d] < left) seen += hist[d--];  // old >= want: it ends by 0
-      s_prefix = prefix | ((uint32_t)d << shift);
-      s_left = left - seen;
+    // thread t: bins 2047 - 2t and 2046 - 2t, so that the sum runs from the top
+    const int hi = kBins - 1 - 2 * tid;
+    const uint32_t h0 = hist[hi], h1 = hist[hi - 1];
+    uint32_t all;
+    const uint32_t above = scan(h0 + h1, s_wave[0], all);
+    if (above < left && left <= above + h0 + h1) {
+      const bool first = left <= above + h0;
+      s_digit = first ? hi : hi - 1;
+      s_left = left - (first ? above : above + h0);
     }
     __syncthreads();
-    prefix = s_prefix;
+    prefix |= s_digit << shift;
     left = s_left;
   }
   // prefix is the smallest key kept, `left` of its rows
-  uint32_t done = 0, ties = 0;
-  for (int i0 = 0; i0 < old; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    const uint32_t k = i < old ? order_key(wt[i]) : 0u;
-    const bool tie = i < old && k == prefix;
-    const uint64_t tmask = __ballot(tie);
-    if (lane == 0) s_wave[0][w] = __popcll(tmask);
-    __syncthreads();
-    uint32_t t = ties, tall = 0;
-    for (int x = 0; x < kSelWaves; ++x) {
-      if (x < w) t += s_wave[0][x];
-      tall += s_wave[0][x];
+  uint32_t done = 0, ties = 0;  // kept, and equal to it, in the tiles before
+  for (int tile = 0; tile < tiles; ++tile) {
+    if (tiles > 1) load(tile);
+    const int i0 = tile * kTileKeys + tid * KPT;
+    uint32_t more = 0, same = 0;
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      more += i0 + j < old && key[j] > prefix;
+      same += i0 + j < old && key[j] == prefix;
     }
-    const uint64_t below = (1ull << lane) - 1;
-    const bool take = i < old && (k > prefix || (tie && t + __popcll(tmask & below) < left));
-    const uint64_t mask = __ballot(take);
-    if (lane == 0) s_wave[1][w] = __popcll(mask);
-    __syncthreads();
-    uint32_t at = done, all = 0;
-    for (int x = 0; x < kSelWaves; ++x) {
-      if (x < w) at += s_wave[1][x];
-      all += s_wave[1][x];
+    uint32_t all_more, all_same;
+    uint32_t t = ties + scan(same, s_wave[0], all_same);
+    uint32_t at = done + scan(more, s_wave[1], all_more) + min(t, left);  // ties before this thread that are kept
+#pragma unroll
+    for (int j = 0; j < KPT; ++j) {
+      if (i0 + j >= old) continue;
+      const bool tie = key[j] == prefix;
+      if (key[j] > prefix || (tie && t < left)) kept[at++] = i0 + j;
+      t += tie;
     }
-    if (take) kept[at + __popcll(mask & below)] = i;
-    done += all;
-    ties += tall;
+    done += all_more;
+    ties += all_same;
     __syncthreads();
   }
 }
@@ -143,7 +214,10 @@ hipError_t launch_cache4_evict(const Cache4EvictArgs& a, hipStream_t stream) {
                       a.max_len,
                       a.budget,
                       a.recent};
-  hipLaunchKernelGGL(cache4_select_kernel, dim3(a.Hkv, a.B), dim3(kSelThreads), 0, stream, p);
+  if (a.max_len <= 4 * kSelThreads)
+    hipLaunchKernelGGL(cache4_select_kernel<4>, dim3(a.Hkv, a.B), dim3(kSelThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL(cache4_select_kernel<16>, dim3(a.Hkv, a.B), dim3(kSelThreads), 0, stream, p);
   const int most = std::min(a.budget, a.max_len);
   if (most > 0) {
     const dim3 grid((most + kMoveRows - 1) / kMoveRows, a.Hkv, a.B);
