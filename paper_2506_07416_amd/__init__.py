@@ -310,24 +310,24 @@ def psm_forward(emb: torch.Tensor, params: torch.Tensor, n_heads: int, d_ff: int
 
 # ------------------------------------------------------------------ the 4-bit cache, drafted tokens
 
-def _arg(name: str, t: torch.Tensor, dtype, shape: tuple, device) -> int:
-    """Address of an argument that has this type, shape and device, densely laid out."""
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got "
-                         f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
-    return t.data_ptr()
+def _arg(name: str, t: torch.Tensor, dtype, shape: tuple, dev: int) -> int:
+    """Address of an argument that has this type, shape and device index (-1: the host), densely laid out."""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on device {dev}, got "
+                     f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
-def _enqueue(call: str, device, *args) -> None:
-    """Runs a call on the current stream of `device`, which need not be the current one."""
-    if device.type != "cuda":
+def _enqueue(call: str, dev: int, *args) -> None:
+    """Runs a call on the current stream of device `dev`, which need not be the current one."""
+    if dev < 0:
         raise ValueError(f"{call}: tensors must live on the GPU")
     fn = getattr(load(), call)
-    if device.index == torch.cuda.current_device():
-        st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if dev == torch.cuda.current_device():
+        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
     else:
-        with torch.cuda.device(device):
-            st = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(dev):
+            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
     if st:
         _abi.check(st, call)
 
@@ -340,6 +340,12 @@ def _float_code(name: str, t: torch.Tensor) -> int:
     raise TypeError(f"{name}: float32 or bfloat16 expected, got {t.dtype}")
 
 
+def _workspace(t: torch.Tensor, dev: int) -> int:
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on device {dev}, got one on {t.device}")
+    return t.data_ptr()
+
+
 def _cache_shape(cache: torch.Tensor, D: int):
     """(B, Hkv, cap) of a cache tensor of head dim D, and its address."""
     if D not in (64, 128):
@@ -348,7 +354,7 @@ def _cache_shape(cache: torch.Tensor, D: int):
     cap, rest = divmod(n, D + D // 16)
     if rest:
         raise ValueError(f"a cache of head dim {D} has {D + D // 16} bytes a position, not {n} for all of them")
-    return B, Hkv, cap, _arg("cache", cache, torch.uint8, (B, Hkv, n), cache.device)
+    return B, Hkv, cap, _arg("cache", cache, torch.uint8, (B, Hkv, n), cache.get_device())
 
 
 def cache4_empty(B: int, Hkv: int, D: int, cap: int, device="cuda") -> torch.Tensor:
@@ -366,11 +372,11 @@ def cache4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_new:
     sample b go to positions start[b].. (at most max_new a sample). weight [B,Hkv,cap] is set to
     0 at those positions."""
     rows, _, D = k.shape
-    dev = k.device
+    dev = cache.get_device()
     B, Hkv, cap, cptr = _cache_shape(cache, D)
     shape = (rows, Hkv, D)
     _enqueue("litevlm_cache4_append", dev, _float_code("k", k), B, Hkv, D, cap, max_new,
-             _arg("k", k, k.dtype, shape, cache.device), _arg("v", v, k.dtype, shape, dev),
+             _arg("k", k, k.dtype, shape, dev), _arg("v", v, k.dtype, shape, dev),
              _arg("cu_new", cu_new, torch.int32, (B + 1,), dev), _arg("start", start, torch.int32, (B,), dev), cptr,
              None if weight is None else _arg("weight", weight, torch.float32, (B, Hkv, cap), dev))
 
@@ -381,10 +387,10 @@ def cache4_read(cache: torch.Tensor, D: int, cu_rows: torch.Tensor, start: torch
     of sample b. Returns (k, v) [rows,Hkv,D]; without `out` they have `rows` rows (B * max_rows by
     default) of `dtype`, and rows past cu_rows[B] are not written."""
     B, Hkv, cap, cptr = _cache_shape(cache, D)
-    dev = cache.device
+    dev = cache.get_device()
     if out is None:
         shape = (B * max_rows if rows is None else rows, Hkv, D)
-        out = (torch.empty(shape, dtype=dtype, device=dev), torch.empty(shape, dtype=dtype, device=dev))
+        out = (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
     k, v = out
     shape = (k.shape[0], Hkv, D)
     _enqueue("litevlm_cache4_read", dev, _float_code("k", k), B, Hkv, D, cap, max_rows, cptr,
@@ -408,10 +414,8 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
     each sample's first weight_rows queries (weight None: 0; weight_out None: in place).
     Returns [rows,Hq,D] in q's type."""
     rows, Hq, D = q.shape
-    dev = q.device
+    dev = cache.get_device()
     B, Hkv, cap, cptr = _cache_shape(cache, D)
-    if cache.device != dev:
-        raise ValueError(f"the cache lives on {cache.device}, the queries on {dev}")
     code = _float_code("q", q)
     if softmax_scale is None:
         softmax_scale = 1.0 / math.sqrt(D)
@@ -429,11 +433,11 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
             wout = _arg("weight_out", weight_out, torch.float32, (B, Hkv, cap), dev)
     if workspace is None:
         n = load().litevlm_cache4_attn_workspace(code, B, Hq, Hkv, D, max_q, max_len, weight_rows)
-        workspace = torch.empty((n or 1,), dtype=torch.uint8, device=dev)
+        workspace = torch.empty((n or 1,), dtype=torch.uint8, device=q.device)
     _enqueue("litevlm_cache4_attn", dev, code, B, Hq, Hkv, D, cap, max_q, max_len, weight_rows,
              _arg("q", q, q.dtype, (rows, Hq, D), dev), _arg("cu_q", cu_q, torch.int32, (B + 1,), dev), cptr,
              _arg("lengths", lengths, torch.int32, (B,), dev), softmax_scale,
-             _arg("out", out, q.dtype, (rows, Hq, D), dev), win, wout, _ptr(workspace), workspace.nbytes)
+             _arg("out", out, q.dtype, (rows, Hq, D), dev), win, wout, _workspace(workspace, dev), workspace.nbytes)
     return out
 
 
@@ -444,19 +448,19 @@ def cache4_evict(cache: torch.Tensor, D: int, weight: torch.Tensor, lengths: tor
     default budget rounded up to 32), weight [B,Hkv,cap_out], lengths [B] and kept_index
     [B,Hkv,budget], all valid up to lengths[b]. ``out`` may supply them under the same keys."""
     B, Hkv, cap, cptr = _cache_shape(cache, D)
-    dev = cache.device
+    dev, device = cache.get_device(), cache.device
     o = dict(out or {})
     if "cache" not in o:
-        o["cache"] = cache4_empty(B, Hkv, D, (budget + 31) // 32 * 32 if cap_out is None else cap_out, dev)
+        o["cache"] = cache4_empty(B, Hkv, D, (budget + 31) // 32 * 32 if cap_out is None else cap_out, device)
     B2, H2, cap_out, optr = _cache_shape(o["cache"], D)
     if (B2, H2) != (B, Hkv):
         raise ValueError(f"the new cache is for {B2} samples and {H2} heads, not {B} and {Hkv}")
     if "weight" not in o:
-        o["weight"] = torch.empty((B, Hkv, cap_out), dtype=torch.float32, device=dev)
+        o["weight"] = torch.empty((B, Hkv, cap_out), dtype=torch.float32, device=device)
     if "lengths" not in o:
-        o["lengths"] = torch.empty((B,), dtype=torch.int32, device=dev)
+        o["lengths"] = torch.empty((B,), dtype=torch.int32, device=device)
     if "kept_index" not in o:
-        o["kept_index"] = torch.empty((B, Hkv, budget), dtype=torch.int32, device=dev)
+        o["kept_index"] = torch.empty((B, Hkv, budget), dtype=torch.int32, device=device)
     _enqueue("litevlm_cache4_evict", dev, B, Hkv, D, cap, cap_out, max_len, budget, recent, cptr,
              _arg("weight", weight, torch.float32, (B, Hkv, cap), dev),
              _arg("lengths", lengths, torch.int32, (B,), dev), optr,
@@ -480,28 +484,28 @@ def verify_draft(draft: torch.Tensor, target: torch.Tensor, proposal: Optional[t
     supply them under the same keys."""
     B, m = draft.shape
     V = target.shape[2]
-    dev = draft.device
+    dev, device = draft.get_device(), draft.device
     code = _float_code("target", target)
     o = dict(out or {})
     if "tokens" not in o:
-        o["tokens"] = torch.empty((B, m + 1), dtype=torch.int32, device=dev)
+        o["tokens"] = torch.empty((B, m + 1), dtype=torch.int32, device=device)
     if "n_accepted" not in o:
-        o["n_accepted"] = torch.empty((B,), dtype=torch.int32, device=dev)
+        o["n_accepted"] = torch.empty((B,), dtype=torch.int32, device=device)
     lin = lout = None
     if lengths is not None:
         lin = _arg("lengths", lengths, torch.int32, (B,), dev)
         if "lengths" not in o:
-            o["lengths"] = torch.empty((B,), dtype=torch.int32, device=dev)
+            o["lengths"] = torch.empty((B,), dtype=torch.int32, device=device)
         lout = _arg("out lengths", o["lengths"], torch.int32, (B,), dev)
     if workspace is None:
         n = load().litevlm_verify_draft_workspace(B, m, V)
-        workspace = torch.empty((n or 1,), dtype=torch.uint8, device=dev)
+        workspace = torch.empty((n or 1,), dtype=torch.uint8, device=device)
     _enqueue("litevlm_verify_draft", dev, code, B, m, V, _arg("draft", draft, torch.int32, (B, m), dev),
              None if n_draft is None else _arg("n_draft", n_draft, torch.int32, (B,), dev),
              _arg("target", target, target.dtype, (B, m + 1, V), dev),
              None if proposal is None else _arg("proposal", proposal, target.dtype, (B, m, V), dev),
              _arg("u", u, torch.float32, (B, m), dev), _arg("r", r, torch.float32, (B,), dev), lin,
              _arg("out tokens", o["tokens"], torch.int32, (B, m + 1), dev),
-             _arg("out n_accepted", o["n_accepted"], torch.int32, (B,), dev), lout, _ptr(workspace),
+             _arg("out n_accepted", o["n_accepted"], torch.int32, (B,), dev), lout, _workspace(workspace, dev),
              workspace.nbytes)
     return o

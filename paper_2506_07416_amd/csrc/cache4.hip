@@ -18,24 +18,30 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = 64;  // rows of a workgroup
 
-// Eight elements of a row, as the bits of fp32 values.
+// Eight elements of a row as they lie in memory, and the bits of their fp32 values.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* base, int64_t elem, uint32_t* x) {
-  if constexpr (BF16) {
-    const uint4 r = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + elem);
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = w[i] << 16;
-      x[2 * i + 1] = w[i] & 0xFFFF0000u;
-    }
-  } else {
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(base) + elem);
-    const uint4 a = p[0], b = p[1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
-    x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+struct Eight {
+  uint4 w[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const void* base, int64_t elem) {
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem * (BF16 ? 2 : 4));
+    w[0] = p[0];
+    if constexpr (!BF16) w[1] = p[1];
   }
-}
+  __device__ __forceinline__ void bits(uint32_t* x) const {
+    const uint32_t a[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
+    if constexpr (BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[2 * i] = a[i] << 16;
+        x[2 * i + 1] = a[i] & 0xFFFF0000u;
+      }
+    } else {
+      const uint32_t b[4] = {w[1].x, w[1].y, w[1].z, w[1].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+    }
+  }
+};
 
 __device__ __forceinline__ uint32_t umax_dpp_quad(uint32_t m) {
   const uint32_t a = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, false);  // lane ^ 1
@@ -91,23 +97,37 @@ __global__ __launch_bounds__(kThreads) void cache4_append_kernel(RowsParams p) {
   const int64_t pos0 = (int64_t)p.start[b] + i0;
   const CacheHead<D> c(p.cache, (int64_t)b * p.Hkv + g, p.cap);
   const int t = tid % LPR;
+  // the rows of kAhead passes are requested before the first is encoded (behind the
+  // last row, that row again)
+  constexpr int kPasses = kTile / RPI, kAhead = BF16 ? (kPasses < 4 ? kPasses : 4) : (kPasses < 2 ? kPasses : 2);
 #pragma unroll
-  for (int it = 0; it < kTile / RPI; ++it) {
-    const int r = it * RPI + tid / LPR;
-    if (i0 + r >= n) continue;  // whole quads: LPR is a multiple of 4
-    const int64_t elem = ((int64_t)(lo + i0 + r) * p.Hkv + g) * D + t * 8;
-    uint32_t x[8], byte;
-    const int64_t pos = pos0 + r;
-    const bool in = pos >= 0 && pos < p.cap;
-    load8<BF16>(p.k_in, elem, x);
-    const uint32_t kw = encode8(x, byte);
-    if ((t & 3) == 0) s_scale[0][t >> 2][r] = (uint8_t)byte;
-    load8<BF16>(p.v_in, elem, x);
-    const uint32_t vw = encode8(x, byte);
-    if ((t & 3) == 0) s_scale[1][t >> 2][r] = (uint8_t)byte;
-    if (in) {
-      reinterpret_cast<uint32_t*>(c.kc + pos * CacheHead<D>::kRow)[t] = kw;
-      reinterpret_cast<uint32_t*>(c.vc + pos * CacheHead<D>::kRow)[t] = vw;
+  for (int it0 = 0; it0 < kPasses; it0 += kAhead) {
+    if (i0 + it0 * RPI >= n) break;
+    Eight<BF16> k[kAhead], v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int row = min(i0 + (it0 + i) * RPI + tid / LPR, n - 1);
+      const int64_t elem = ((int64_t)(lo + row) * p.Hkv + g) * D + t * 8;
+      k[i].load(p.k_in, elem);
+      v[i].load(p.v_in, elem);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int r = (it0 + i) * RPI + tid / LPR;
+      const int64_t pos = pos0 + r;
+      uint32_t x[8], kb, vb;
+      k[i].bits(x);
+      const uint32_t kw = encode8(x, kb);
+      v[i].bits(x);
+      const uint32_t vw = encode8(x, vb);
+      if ((t & 3) == 0) {
+        s_scale[0][t >> 2][r] = (uint8_t)kb;
+        s_scale[1][t >> 2][r] = (uint8_t)vb;
+      }
+      if (i0 + r < n && pos >= 0 && pos < p.cap) {
+        reinterpret_cast<uint32_t*>(c.kc + pos * CacheHead<D>::kRow)[t] = kw;
+        reinterpret_cast<uint32_t*>(c.vc + pos * CacheHead<D>::kRow)[t] = vw;
+      }
     }
   }
   __syncthreads();

@@ -477,42 +477,49 @@ __global__ __launch_bounds__(kThreads) void cache4_join_kernel(AttnParams p, int
     return;
   }
   __shared__ float2 s_stat[kKept];
+  const int k0 = (((int)blockIdx.x - joins) * kThreads + tid) * 4;
+  if (k0 - tid * 4 >= sm.n) return;
   const int rows = min(sm.rows, p.wrows);
-  if (((int)blockIdx.x - joins) * kThreads * 4 >= sm.n) return;
+  const int64_t at = head * p.cap + k0;
+  const bool live = k0 < sm.n;
+  const auto vec = [&](const float* q) { return k0 + 4 <= sm.n && (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
+  f32x4 w = {0.f, 0.f, 0.f, 0.f}, x[kKept];
+  // requested before the statistics; rows that do not see the keys may not have
+  // written them: their numbers are not used
+#pragma unroll
+  for (int r = 0; r < kKept; ++r)
+    if (live && r < rows) x[r] = *reinterpret_cast<const f32x4*>(p.logit + (head * p.wrows + r) * p.lpad + k0);
+  if (live && p.weight_in) {
+    if (vec(p.weight_in)) {
+      w = *reinterpret_cast<const f32x4*>(p.weight_in + at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (k0 + i < sm.n) w[i] = p.weight_in[at + i];
+    }
+  }
   for (int r = tid >> 6; r < rows; r += kWaves) {
     const float2 st = join_stat(p.part_ml + (head * p.rows + r) * p.nsplit, live_splits<MT>(p, sm, r), sm.seen(p, r) > 0);
     if ((tid & 63) == 0) s_stat[r] = st;
   }
-  const int k0 = (((int)blockIdx.x - joins) * kThreads + tid) * 4;
-  const int64_t at = head * p.cap + k0;
-  const bool live = k0 < sm.n;
-  const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-  float4 w = zero, x[kKept];
-  if (live) {
-    // rows that do not see the keys may not have written them: their numbers are not used
-    #pragma unroll
-    for (int r = 0; r < kKept; ++r)
-      x[r] = r < rows ? *reinterpret_cast<const float4*>(p.logit + (head * p.wrows + r) * p.lpad + k0) : zero;
-    if (p.weight_in) {
-      // cap is a multiple of 4 and the rows end inside it; the address may be any float's
-      w = make_float4(p.weight_in[at], p.weight_in[at + 1], p.weight_in[at + 2], p.weight_in[at + 3]);
-    }
-  }
   __syncthreads();
   if (!live) return;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int r = 0; r < kKept; ++r) {
-    const int seen = r < rows ? sm.seen(p, r) : 0;
+    if (r >= rows) break;
+    const int seen = sm.seen(p, r);
     const float2 st = s_stat[r];
-    const float y[4] = {x[r].x, x[r].y, x[r].z, x[r].w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] += k0 + i < seen ? __builtin_amdgcn_exp2f(y[i] - st.x) * st.y : 0.f;
+    for (int i = 0; i < 4; ++i) s[i] += k0 + i < seen ? __builtin_amdgcn_exp2f(x[r][i] - st.x) * st.y : 0.f;
   }
-  const float v[4] = {w.x + s[0], w.y + s[1], w.z + s[2], w.w + s[3]};
+  if (vec(p.weight_out)) {
+    *reinterpret_cast<f32x4*>(p.weight_out + at) = w + s;
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (k0 + i < sm.n) p.weight_out[at + i] = v[i];
+    for (int i = 0; i < 4; ++i)
+      if (k0 + i < sm.n) p.weight_out[at + i] = w[i] + s[i];
+  }
 }
 
 // The same, the logits taken again: one wave, 16 keys.
