@@ -28,7 +28,6 @@ constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kKeys = 32;              // keys of a wave's step
 constexpr int kStep = kWaves * kKeys;  // keys of a workgroup's step
 constexpr int kKept = 8;               // rows of a KV head whose logits are kept
-constexpr int64_t kGroupsWanted = 512;  // workgroups of the first kernel, where the keys allow
 constexpr float kSlack = 8.f;          // the running reference may lag the maximum by this (log2)
 
 struct AttnParams {
@@ -295,6 +294,7 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
         const uint8_t* sc = c.vs + ((uint32_t)(lg * D / 128) * (uint32_t)p.cap + k0);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
+#pragma unroll 1
           for (int kk = 0; kk < kKeys; ++kk)
             if (k0 + kk < seen[mt] && sc[kk] == 255u) bad |= 1u << mt;
       }
@@ -305,7 +305,11 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
       float x[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][mt][i & 3];
-      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      // three at a time; a NaN stays one, compares false below, and spoils the sum
+      const auto max3 = [](float a, float b, float c) __attribute__((always_inline)) {
+        return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+      };
+      float top = __builtin_elementwise_maximum(max3(max3(x[0], x[1], x[2]), x[3], x[4]), max3(x[5], x[6], x[7]));
       top *= p.scale_log2;
       if (__any(top > ref[mt] + kSlack)) {
         top = fmaxf(ref[mt], max_xor32(max_xor16(top)));
@@ -564,7 +568,7 @@ __global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
 
 // Row tiles of a workgroup. Two decode a key once for 32 rows; four would hold 128
 // registers of outputs and leave one wave a SIMD (256 queries of 4 heads over 6528
-// rows: 2 tiles 47 us, 4 tiles 61 us, 1 tile 57 us).
+// rows: 2 tiles 46-48 us, 4 tiles 61 us, 1 tile 57 us).
 int row_tiles(int64_t rows) { return rows <= 16 ? 1 : 2; }
 
 // Keeping the logits of a row costs 8 bytes a key (written and read), taking them
@@ -607,15 +611,17 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   const int64_t rows = (int64_t)max_q * G, wrows = (int64_t)weight_rows * G, heads = (int64_t)B * Hkv;
   const int per = 16 * row_tiles(rows);
   lay.blocks = (int)((rows + per - 1) / per);
-  // Splits of whole steps of 128 keys: two workgroups a CU where there are keys for
-  // them (a ragged batch of 8 x 3200 rows, 5 queries: 512 workgroups 14.4 us, 1024
-  // 15.8 us, 1664 19.5 us: a short split's start and end cost more than its keys).
-  // With one row tile memory is the bound, and splits of 512 keys let the CUs finish
-  // together (32 samples of 10-16K rows: 512 keys 101 us, 1024 106 us, 2048 112 us,
-  // 4096 117 us).
+  // Splits of whole steps of 128 keys. With one row tile memory is the bound: two
+  // workgroups a CU, and splits of at most 512 keys, so that the CUs finish together
+  // (32 samples of 10-16K rows: 512 keys 101 us, 1024 106 us, 2048 112 us, 4096 117
+  // us). With two the issue of instructions is: one workgroup a CU, since a split's
+  // start and end cost more than its keys and its part has to be joined (8 samples
+  // of 3200 rows, 5 queries: 256 workgroups 13.2 us, 512 14.3, 1664 19.5; 256 queries:
+  // 256 workgroups, no split, 48 us; 512 46 us and 12 us to join).
   const int64_t groups = std::max<int64_t>(heads * lay.blocks, 1);
   const int64_t steps = std::max((max_len + kStep - 1) / kStep, 1);
-  int64_t want = (kGroupsWanted + groups - 1) / groups;
+  const int64_t aim = per == 16 ? 512 : 256;  // workgroups
+  int64_t want = (aim + groups - 1) / groups;
   if (per == 16) want = std::max(want, (steps + 3) / 4);
   want = std::min(want, steps);
   const int64_t each = (steps + want - 1) / want;
