@@ -572,7 +572,7 @@ size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32
  * A query that sees no row (m_b > n_b) gives o = 0 and adds no weight. Softmax and
  * accumulation in fp32. For bf16 queries the probabilities are rounded to bf16
  * in front of the product with V (the weights and the softmax sum are not); for
- * fp32 queries every product is exact in fp32. A probability below 2^-126 of its
+ * fp32 queries (of 2^-100 and more) every product is exact in fp32. A probability below 2^-126 of its
  * row's largest counts as 0.
  *
  *   dtype              LITEVLM_F32 or LITEVLM_BF16 (q and o)
@@ -586,7 +586,7 @@ size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32
  *   cu_q               dev int32 [B+1], non-decreasing, cu_q[0] = 0
  *   lengths            dev int32 [B]
  *   softmax_scale      finite, > 0
- *   o                  dev out [total, Hq, D]; rows past total are untouched
+ *   o                  dev out [total, Hq, D], not over q; rows past total are untouched
  *   weight_in          dev fp32 [B, Hkv, cap], or NULL = 0 (ignored when weight_rows is 0)
  *   weight_out         dev out fp32 [B, Hkv, cap], required when weight_rows > 0 (may be
  *                      weight_in): written for j < n_b, untouched behind
@@ -676,6 +676,7 @@ size_t litevlm_verify_draft_workspace(int32_t B, int32_t max_draft, int32_t V);
  *                      lengths[b] - (n - a), the rows that stay valid
  *   workspace          dev scratch of litevlm_verify_draft_workspace() bytes (contents on
  *                      entry ignored; calls that may run concurrently must not share one)
+ * Except for lengths_out, no output may overlap an input.
  */
 litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draft, int32_t V,
                                       const int32_t* draft, const int32_t* n_draft, const void* target,

@@ -11,7 +11,7 @@ using namespace litevlm;
 
 namespace {
 
-constexpr int32_t kVersion = 100;  // 0.1.0
+constexpr int32_t kVersion = 200;  // 0.2.0
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 bool finite_pos(float x) { return isfinite(x) && x > 0.f; }
@@ -614,7 +614,7 @@ litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32
   if (st != LITEVLM_OK) return st;
   if (max_len > cap) return LITEVLM_ERR_BAD_SHAPE;
   if (weight_rows > 0 && !weight_out) return LITEVLM_ERR_NULL_POINTER;
-  if (!finite_pos(softmax_scale)) return LITEVLM_ERR_BAD_VALUE;
+  if (!finite_pos(softmax_scale) || o == q) return LITEVLM_ERR_BAD_VALUE;
   const void* big[] = {q, cache, o, workspace};
   for (const void* p : big)
     if (p && !aligned(p, 16)) return LITEVLM_ERR_MISALIGNED;

@@ -622,7 +622,8 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   const int64_t steps = std::max((max_len + kStep - 1) / kStep, 1);
   const int64_t aim = per == 16 ? 512 : 256;  // workgroups
   int64_t want = (aim + groups - 1) / groups;
-  if (per == 16) want = std::max(want, (steps + 3) / 4);
+  // at most 16384 workgroups: a part takes 4 * D bytes a row of the workspace
+  if (per == 16) want = std::max(want, std::min<int64_t>((steps + 3) / 4, (16384 + groups - 1) / groups));
   want = std::min(want, steps);
   const int64_t each = (steps + want - 1) / want;
   lay.split_len = (int)(each * kStep);

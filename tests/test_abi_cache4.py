@@ -76,7 +76,7 @@ def test_attn_refusals():
                 dict(B=256, mq=_abi.MAX_CACHE4)):
         assert attn(**bad) == _abi.ERR_BAD_SHAPE, bad
     for bad in (dict(wr=-1), dict(wr=5), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")),
-                dict(scale=-1.0)):
+                dict(scale=-1.0), dict(o=at(0))):
         assert attn(**bad) == _abi.ERR_BAD_VALUE, bad
     for name in ("q", "cache", "o", "ws"):
         assert attn(**{name: A + 8}) == _abi.ERR_MISALIGNED

@@ -191,10 +191,14 @@ def test_attention_matches_oracle(case):
     ws.fill_(0x7F)
     o2 = lv.cache4_attn(*args, weight=wt, weight_rows=wr, workspace=ws)
     assert torch.equal(o2[:cu[-1]], o[:cu[-1]]) and torch.equal(wt, wo)
+    odd = torch.zeros((B * H * cap + 1,), device="cuda")[1:].view(B, H, cap)
+    odd.copy_(torch.as_tensor(weight))
+    lv.cache4_attn(*args, weight=odd, weight_rows=wr)
+    assert torch.equal(odd, wo)
     o3 = lv.cache4_attn(*args)
     assert torch.equal(o3[:cu[-1]], o[:cu[-1]])
-    # weights from nothing
-    fresh = torch.zeros((B, H, cap), device="cuda")
+    # weights from nothing, at an address not aligned to 16 bytes
+    fresh = torch.zeros((B * H * cap + 1,), device="cuda")[1:].view(B, H, cap)
     lv.cache4_attn(*args, weight_out=fresh, weight_rows=wr)
     check_attn(cache, q, cu, lens, Hq, D, dtype, wr, np.zeros((B, H, cap)), got[:cu[-1]],
                fresh.double().cpu().numpy(), f"case {case}, from nothing")
@@ -323,6 +327,7 @@ EVICT = [
     ([3000, 2999, 1025], 1024, 100, 2, 64, 3008, 1024, 0),
     ([5000], 4999, 4998, 1, 128, 5024, 5024, 0),
     ([2048, 2047], 1, 1, 2, 64, 2048, 32, 0),
+    ([40000, 16385, 32768], 9000, 77, 1, 64, 40000, 9024, 0),     # more keys than a workgroup holds at once
 ]
 
 
@@ -340,7 +345,9 @@ def test_evict_matches_oracle(case, ties):
     co = rng.integers(0, 256, (B, H, cap_out * (D + D // 16))).astype(np.uint8)
     out = dict(cache=torch.as_tensor(co).cuda(), weight=torch.full((B, H, cap_out), 5.0, device="cuda"),
                kept_index=torch.full((B, H, budget), -7, dtype=torch.int32, device="cuda"))
-    r = lv.cache4_evict(torch.as_tensor(cache).cuda(), D, torch.as_tensor(w).cuda(), dev(lens), budget, recent,
+    wt = torch.zeros((w.size + 1,), device="cuda")[1:].view(w.shape) if case % 2 else torch.zeros(w.shape, device="cuda")
+    wt.copy_(torch.as_tensor(w))              # every other case: not aligned to 16 bytes
+    r = lv.cache4_evict(torch.as_tensor(cache).cuda(), D, wt, dev(lens), budget, recent,
                         min(cap, max(lens) + extra), out=out)
     src, dst, old = (c4.split_cache(x, D) for x in (cache, r["cache"].cpu().numpy(), co))
     kept, wo = r["kept_index"].cpu().numpy(), r["weight"].cpu().numpy()
