@@ -318,16 +318,20 @@ def _arg(name: str, t: torch.Tensor, dtype, shape: tuple, dev: int) -> int:
                      f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
+# the current stream's handle without a Stream object around it (1 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
+
+
 def _enqueue(call: str, dev: int, *args) -> None:
     """Runs a call on the current stream of device `dev`, which need not be the current one."""
     if dev < 0:
         raise ValueError(f"{call}: tensors must live on the GPU")
     fn = getattr(load(), call)
     if dev == torch.cuda.current_device():
-        st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+        st = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
-            st = fn(*args, torch.cuda.current_stream(dev).cuda_stream)
+            st = fn(*args, _raw_stream(dev))
     if st:
         _abi.check(st, call)
 

@@ -16,29 +16,28 @@ namespace litevlm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTile = 64;  // rows of a workgroup
+constexpr int kTile = 32;  // rows of a workgroup (1M rows read back: 32 116 us, 64 122 us)
 
 // Eight elements of a row as they lie in memory, and the bits of their fp32 values.
 template <bool BF16>
 struct Eight {
-  uint4 w[BF16 ? 1 : 2];
+  i32x4 w[BF16 ? 1 : 2];
+  // read once and never again: past the caches (20.7K rows of 8 heads 30 -> 20 us)
   __device__ __forceinline__ void load(const void* base, int64_t elem) {
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(base) + elem * (BF16 ? 2 : 4));
-    w[0] = p[0];
-    if constexpr (!BF16) w[1] = p[1];
+    const i32x4* p = reinterpret_cast<const i32x4*>(static_cast<const uint8_t*>(base) + elem * (BF16 ? 2 : 4));
+    w[0] = __builtin_nontemporal_load(p);
+    if constexpr (!BF16) w[1] = __builtin_nontemporal_load(p + 1);
   }
   __device__ __forceinline__ void bits(uint32_t* x) const {
-    const uint32_t a[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
-    if constexpr (BF16) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[2 * i] = a[i] << 16;
-        x[2 * i + 1] = a[i] & 0xFFFF0000u;
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
+        x[2 * i] = (uint32_t)w[0][i] << 16;
+        x[2 * i + 1] = (uint32_t)w[0][i] & 0xFFFF0000u;
+      } else {
+        x[i] = (uint32_t)w[0][i];
+        x[4 + i] = (uint32_t)w[1][i];
       }
-    } else {
-      const uint32_t b[4] = {w[1].x, w[1].y, w[1].z, w[1].w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
     }
   }
 };
@@ -83,7 +82,7 @@ struct RowsParams {
   int Hkv, cap, max_rows;
 };
 
-// One workgroup: 64 rows of one head, K and V; lane t of D/8 holds elements
+// One workgroup: 32 rows of one head, K and V; lane t of D/8 holds elements
 // [8t, 8t + 8) of a row, so the four lanes of a block are a quad. The scales are
 // gathered in LDS, since those of consecutive rows lie side by side in the cache.
 template <int D, bool BF16>
@@ -142,18 +141,21 @@ __global__ __launch_bounds__(kThreads) void cache4_append_kernel(RowsParams p) {
   if (p.weight && tid < kTile) p.weight[((int64_t)b * p.Hkv + g) * p.cap + pos] = 0.f;
 }
 
+// Past the caches, for the sake of what lies in them: the rows of an eviction that
+// is read back, 16 samples of 8192 rows, move in 62 instead of 78 us, and are read
+// in 122 instead of 128.
 template <bool BF16>
 __device__ __forceinline__ void store8(void* base, int64_t elem, uint32_t w, float scale) {
   if constexpr (BF16) {
-    *reinterpret_cast<bf16x8*>(static_cast<uint16_t*>(base) + elem) = decode8(w, scale);
+    __builtin_nontemporal_store(__builtin_bit_cast(i32x4, decode8(w, scale)), reinterpret_cast<i32x4*>(static_cast<uint16_t*>(base) + elem));
   } else {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(base) + elem);
+    f32x4* o = reinterpret_cast<f32x4*>(static_cast<float*>(base) + elem);
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
     const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
     const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2);
     const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-    o[0] = make_float4(a[0], a[1], b[0], b[1]);
-    o[1] = make_float4(c[0], c[1], d[0], d[1]);
+    __builtin_nontemporal_store(f32x4{a[0], a[1], b[0], b[1]}, o);
+    __builtin_nontemporal_store(f32x4{c[0], c[1], d[0], d[1]}, o + 1);
   }
 }
 
