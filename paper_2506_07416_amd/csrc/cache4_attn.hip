@@ -120,15 +120,14 @@ struct Attn {
     uint32_t w[kSteps];
     uint32_t scale;
   };
+  template <bool ONCE>
   static __device__ __forceinline__ void load_key(const CacheHead<D>& c, int cap, int k0, int lg, int col, Key& k) {
     const uint8_t* src = c.kc + ((uint32_t)(k0 + col) * (D / 2) + lg * (D / 8));
-    if constexpr (D == 128) {
-      const uint4 x = *reinterpret_cast<const uint4*>(src);
-      k.w[0] = x.x, k.w[1] = x.y, k.w[2] = x.z, k.w[3] = x.w;
-    } else {
-      const uint2 x = *reinterpret_cast<const uint2*>(src);
-      k.w[0] = x.x, k.w[1] = x.y;
-    }
+    typedef uint32_t words __attribute__((ext_vector_type(kSteps)));
+    const words* row = reinterpret_cast<const words*>(src);
+    const words x = ONCE ? __builtin_nontemporal_load(row) : *row;
+#pragma unroll
+    for (int t = 0; t < kSteps; ++t) k.w[t] = x[t];
     k.scale = c.ks[(uint32_t)(lg * D / 128) * (uint32_t)cap + k0 + col];
   }
   // Logits (without the scale) of 16 * MT rows against those keys.
@@ -205,7 +204,7 @@ struct Attn {
 // follows its maximum only when a logit exceeds it by kSlack: until then the
 // probabilities are at most 2^kSlack, and neither an exchange between lanes nor a
 // rescaling of the output is needed.
-template <int D, int TERMS, int MT, bool KEEP>
+template <int D, int TERMS, int MT, bool KEEP, bool ONCE>
 __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache4_attn_kernel(AttnParams p) {
   using A = Attn<D, TERMS>;
   constexpr int LD = D + 4;  // row of the joining buffer: 16 rows start in different banks
@@ -249,16 +248,16 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
   typename A::Value vn;
   int k0 = begin + wave * kKeys;
   if (k0 < end) {
-    A::load_key(c, p.cap, k0, lg, col, kn[0]);
-    A::load_key(c, p.cap, k0 + 16, lg, col, kn[1]);
+    A::template load_key<ONCE>(c, p.cap, k0, lg, col, kn[0]);
+    A::template load_key<ONCE>(c, p.cap, k0 + 16, lg, col, kn[1]);
     A::load_value(c, p.cap, k0, lg, col, vn);
   }
   for (; k0 < end; k0 += kStep) {
     const typename A::Key kc[2] = {kn[0], kn[1]};
     typename A::Value vc = vn;
     if (k0 + kStep < end) {
-      A::load_key(c, p.cap, k0 + kStep, lg, col, kn[0]);
-      A::load_key(c, p.cap, k0 + kStep + 16, lg, col, kn[1]);
+      A::template load_key<ONCE>(c, p.cap, k0 + kStep, lg, col, kn[0]);
+      A::template load_key<ONCE>(c, p.cap, k0 + kStep + 16, lg, col, kn[1]);
       A::load_value(c, p.cap, k0 + kStep, lg, col, vn);
     }
     f32x4 s[2][MT];
@@ -538,7 +537,7 @@ __global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
   const int64_t head = (int64_t)b * p.Hkv + g;
   const CacheHead<D> c(p.cache, head, p.cap);
   typename A::Key kn;
-  A::load_key(c, p.cap, k0, lg, col, kn);
+  A::template load_key<false>(c, p.cap, k0, lg, col, kn);
   float w[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r0 = 0; r0 < rows; r0 += 16) {
     const int r = r0 + col;
@@ -579,8 +578,18 @@ template <int D, int TERMS, int MT>
 void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
   const bool weights = p.weight_rows > 0 && p.max_len > 0, keep = weights && keep_logits(p.wrows);
   const dim3 grid(p.Hkv * p.blocks * p.nsplit, B);
-  if (keep) hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS, MT, true>), grid, dim3(kThreads), 0, stream, p);
-  else hipLaunchKernelGGL((cache4_attn_kernel<D, TERMS, MT, false>), grid, dim3(kThreads), 0, stream, p);
+  // keys of more caches than the last-level cache holds half of, each read by one
+  // workgroup, pass it by (493 MB of 32 samples: 119 -> 113 us with the join; at
+  // 3.7 MB, which stay in it, 4.6 -> 5.0 us)
+  const bool once = p.blocks == 1 && CacheHead<D>::bytes(p.max_len) * p.Hkv * B > ((int64_t)128 << 20);
+  const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p); };
+  if (keep) {
+    if (once) run(cache4_attn_kernel<D, TERMS, MT, true, true>);
+    else run(cache4_attn_kernel<D, TERMS, MT, true, false>);
+  } else {
+    if (once) run(cache4_attn_kernel<D, TERMS, MT, false, true>);
+    else run(cache4_attn_kernel<D, TERMS, MT, false, false>);
+  }
   const int joins = p.nsplit > 1 ? p.rows : 0, chunks = keep ? (p.max_len + 4 * kThreads - 1) / (4 * kThreads) : 0;
   if (joins + chunks > 0)
     hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3(joins + chunks, p.Hkv, B), dim3(kThreads), 0, stream, p,
