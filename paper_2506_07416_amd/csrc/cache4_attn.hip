@@ -525,44 +525,78 @@ __global__ __launch_bounds__(kThreads) void cache4_join_kernel(AttnParams p, int
   }
 }
 
-// The same, the logits taken again: one wave, 16 keys.
+// The same, the logits taken again: a wave has 64 keys, decoded once, and goes
+// through the rows 16 at a time, the next ones on their way (36 rows, 8 samples of
+// 3200 rows: 16 keys a wave 15.8 us, 64 keys 12.1 us; 64 rows, 4 of 16300: 56 and
+// 31 us).
+constexpr int kAgainKeys = 64;
 template <int D, int TERMS>
-__global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
+__global__ __launch_bounds__(kThreads) void cache4_weight_again_kernel(AttnParams p) {
   using A = Attn<D, TERMS>;
-  const int b = blockIdx.z, g = blockIdx.y, lane = threadIdx.x, lg = lane >> 4, col = lane & 15;
+  constexpr int KT = kAgainKeys / 16;
+  const int b = blockIdx.z, g = blockIdx.y, lane = threadIdx.x & 63, lg = lane >> 4, col = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Sample sm(p, b);
-  const int k0 = blockIdx.x * 16;
+  const int k0 = (blockIdx.x * kWaves + wave) * kAgainKeys;
   if (k0 >= sm.n) return;
   const int rows = min(sm.rows, p.wrows);
   const int64_t head = (int64_t)b * p.Hkv + g;
   const CacheHead<D> c(p.cache, head, p.cap);
-  typename A::Key kn;
-  A::template load_key<false>(c, p.cap, k0, lg, col, kn);
-  float w[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int r0 = 0; r0 < rows; r0 += 16) {
+  typename A::Key kn[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)  // cap is a multiple of 32: the tiles behind it are not there
+    A::template load_key<false>(c, p.cap, min(k0 + 16 * t, p.cap - 16), lg, col, kn[t]);
+  bf16x8 kf[KT][A::kSteps];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int i = 0; i < A::kSteps; ++i) kf[t][i] = decode8(kn[t].w[i], e8m0_scale(kn[t].scale));
+  float w[KT][4];
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[t][i] = 0.f;
+
+  typename A::Rows next;
+  float2 st_next = make_float2(0.f, 0.f);
+  const auto request = [&](int r0) __attribute__((always_inline)) {
     const int r = r0 + col;
     const bool live = r < rows;
-    const int seen = live ? sm.seen(p, r) : 0;
-    typename A::Rows f;
-    A::load_rows(p, live ? sm.qrow(p, g, r) : 0, live, lg, f);
-    const float2 st = live ? p.stat[head * p.wrows + r] : make_float2(0.f, 0.f);
-    f32x4 s;
-    A::template logits<1>(kn, &f, &s);
+    A::load_rows(p, live ? sm.qrow(p, g, r) : 0, live, lg, next);
+    st_next = live ? p.stat[head * p.wrows + r] : make_float2(0.f, 0.f);
+  };
+  if (rows > 0) request(0);
+  for (int r0 = 0; r0 < rows; r0 += 16) {
+    const typename A::Rows f = next;
+    const float2 st = st_next;
+    if (r0 + 16 < rows) request(r0 + 16);
+    const int r = r0 + col;
+    const int seen = r < rows ? sm.seen(p, r) : 0;
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < A::kSteps; ++i)
+#pragma unroll
+        for (int n = TERMS - 1; n >= 0; --n) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][i], f.q[i][n], s, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -st.x)) * st.y;
+        w[t][i] += k0 + 16 * t + 4 * lg + i < seen ? e : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -st.x)) * st.y;
-      w[i] += k0 + 4 * lg + i < seen ? e : 0.f;
+      const float y = row16_sum(w[t][i]);
+      const int key = k0 + 16 * t + 4 * lg + i;
+      if (col == 0 && key < sm.n) {
+        const int64_t at = head * p.cap + key;
+        p.weight_out[at] = (p.weight_in ? p.weight_in[at] : 0.f) + y;
+      }
     }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float y = row16_sum(w[i]);
-    const int key = k0 + 4 * lg + i;
-    if (col == 0 && key < sm.n) {
-      const int64_t at = head * p.cap + key;
-      p.weight_out[at] = (p.weight_in ? p.weight_in[at] : 0.f) + y;
-    }
-  }
 }
 
 // Row tiles of a workgroup. Two decode a key once for 32 rows; four would hold 128
@@ -571,7 +605,9 @@ __global__ __launch_bounds__(64) void cache4_weight_again_kernel(AttnParams p) {
 int row_tiles(int64_t rows) { return rows <= 16 ? 1 : 2; }
 
 // Keeping the logits of a row costs 8 bytes a key (written and read), taking them
-// again D/2 + D/32 bytes a key for all of them.
+// again D/2 + D/32 bytes a key for all of them, and a launch (8 samples of 3200 rows,
+// the whole call: 4 rows 16.1 us kept, 24.1 again; 8 rows 18.7 and 23.8; 12 rows
+// 30.1 and 23.9; 4 samples of 16300 rows: 8 rows 28.4 and 43.6, 12 rows 53 and 42).
 bool keep_logits(int wrows) { return wrows <= kKept; }
 
 template <int D, int TERMS, int MT>
@@ -595,8 +631,7 @@ void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
     hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3(joins + chunks, p.Hkv, B), dim3(kThreads), 0, stream, p,
                        joins);
   if (weights && !keep)
-    hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>), dim3((p.max_len + 15) / 16, p.Hkv, B), dim3(64), 0,
-                       stream, p);
+    hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>), dim3((p.max_len + kWaves * kAgainKeys - 1) / (kWaves * kAgainKeys), p.Hkv, B), dim3(kThreads), 0, stream, p);
 }
 
 template <int D>
