@@ -27,6 +27,7 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kKeys = 32;              // keys of a wave's step
 constexpr int kStep = kWaves * kKeys;  // keys of a workgroup's step
+constexpr int kFewSplits = 4;          // splits of a row that one thread joins
 constexpr int kKept = 8;               // rows of a KV head whose logits are kept
 constexpr float kSlack = 8.f;          // the running reference may lag the maximum by this (log2)
 
@@ -418,65 +419,78 @@ __device__ __forceinline__ float2 join_stat(const float2* ml, int ns, bool some)
   return make_float2(base, some ? 1.f / l : 0.f);
 }
 
-// Two kinds of workgroup. The first p.rows of a KV head (where the keys were
-// split) join one row's splits: thread (slot, piece) sums 16 bytes of splits slot,
-// slot + SLOTS, ..., the slots are then summed in order. The others (where the
-// logits were kept) take the weight of 1024 keys each.
+// Four elements of an output row.
+template <int TERMS>
+__device__ __forceinline__ void store4(void* o, int64_t at, const f32x4& y) {
+  if constexpr (TERMS == 3) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(o) + at) = y;
+  } else {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(o) + at) = bf16x4{(__bf16)y[0], (__bf16)y[1], (__bf16)y[2], (__bf16)y[3]};
+  }
+}
+
+// Two kinds of workgroup. The first `joins` of a KV head (where the keys were
+// split) join the splits of rows, a thread 16 bytes of them. Up to kFewSplits splits:
+// SLOTS rows a workgroup, a slot of threads each. More: one row, slot k sums splits
+// k, k + SLOTS, ..., then the slots are summed in order. The other workgroups (where
+// the logits were kept) take the weight of 1024 keys each.
 template <int D, int TERMS, int MT>
 __global__ __launch_bounds__(kThreads) void cache4_join_kernel(AttnParams p, int joins) {
-  constexpr int V4 = D / 4, SLOTS = kThreads / V4;
+  constexpr int V4 = D / 4, SLOTS = kThreads / V4, R = kFewSplits;
   const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   const Sample sm(p, b);
   const int64_t head = (int64_t)b * p.Hkv + g;
   if ((int)blockIdx.x < joins) {
-    __shared__ float4 s_part[SLOTS][V4];
-    const int r = blockIdx.x;
-    if (r >= sm.rows) return;
+    __shared__ f32x4 s_part[SLOTS][V4];
+    const bool few = p.nsplit <= kFewSplits;
+    const int slot = tid / V4, c = tid % V4;
+    const int r = few ? blockIdx.x * SLOTS + slot : blockIdx.x;
+    if (r >= sm.rows) return;  // uniform where there is a barrier below
     const int ns = live_splits<MT>(p, sm, r);
     const bool some = sm.seen(p, r) > 0;
     const int64_t at = (head * p.rows + r) * p.nsplit;
     const float2* ml = p.part_ml + at;
-    const float4* po = reinterpret_cast<const float4*>(p.part_o + at * D);
-    const int slot = tid / V4, c = tid % V4;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    const f32x4* po = reinterpret_cast<const f32x4*>(p.part_o + at * D);
+    const int s0 = few ? 0 : slot, step = few ? 1 : SLOTS;
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
     // the first of the thread's splits are requested before the sum is known
-    constexpr int R = 4;
-    float4 x[R];
-    float m[R];
+    f32x4 x[R];
+    float2 m[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
-      const int s = min(slot + i * SLOTS, ns - 1);
+      const int s = min(s0 + i * step, ns - 1);
       x[i] = po[s * V4 + c];
-      m[i] = ml[s].x;
+      m[i] = ml[s];
     }
-    const float2 st = join_stat(ml, ns, some);
-    const auto add = [&](float w, const float4& z) __attribute__((always_inline)) {
-      y.x = fmaf(w, z.x, y.x), y.y = fmaf(w, z.y, y.y), y.z = fmaf(w, z.z, y.z), y.w = fmaf(w, z.w, y.w);
-    };
+    float2 st;
+    if (few) {
+      float top = m[0].x, l = 0.f;
+#pragma unroll
+      for (int i = 1; i < R; ++i) top = fmaxf(top, m[i].x);  // repeats of the last split change no maximum
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        if (i < ns) l = fmaf(__builtin_amdgcn_exp2f(m[i].x - base), m[i].y, l);
+      st = make_float2(base, some ? 1.f / l : 0.f);
+    } else {
+      st = join_stat(ml, ns, some);
+    }
 #pragma unroll
     for (int i = 0; i < R; ++i)
-      if (slot + i * SLOTS < ns) add(__builtin_amdgcn_exp2f(m[i] - st.x), x[i]);
+      if (s0 + i * step < ns) y += __builtin_amdgcn_exp2f(m[i].x - st.x) * x[i];
+    if (!few) {
 #pragma unroll 4
-    for (int s = slot + R * SLOTS; s < ns; s += SLOTS) add(__builtin_amdgcn_exp2f(ml[s].x - st.x), po[(int64_t)s * V4 + c]);
-    s_part[slot][c] = y;
-    __syncthreads();
-    if (tid < V4) {
-      float4 t = s_part[0][tid];
+      for (int s = slot + R * SLOTS; s < ns; s += SLOTS) y += __builtin_amdgcn_exp2f(ml[s].x - st.x) * po[(int64_t)s * V4 + c];
+      s_part[slot][c] = y;
+      __syncthreads();
+      if (slot > 0) return;
 #pragma unroll
-      for (int k = 1; k < SLOTS; ++k) {
-        const float4 u = s_part[k][tid];
-        t.x += u.x, t.y += u.y, t.z += u.z, t.w += u.w;
-      }
-      const float z[4] = {t.x, t.y, t.z, t.w};
-      const int64_t to = sm.qrow(p, g, r) * D + tid * 4;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v = some ? z[e] * st.y : 0.f;
-        if constexpr (TERMS == 3) static_cast<float*>(p.o)[to + e] = v;
-        else static_cast<__bf16*>(p.o)[to + e] = (__bf16)v;
-      }
-      if (tid == 0 && r < p.wrows) p.stat[head * p.wrows + r] = st;
+      for (int k = 1; k < SLOTS; ++k) y += s_part[k][c];
     }
+    const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    store4<TERMS>(p.o, sm.qrow(p, g, r) * D + c * 4, some ? y * st.y : zero);
+    if (c == 0 && r < p.wrows) p.stat[head * p.wrows + r] = st;
     return;
   }
   __shared__ float2 s_stat[kKept];
@@ -626,7 +640,9 @@ void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
     if (once) run(cache4_attn_kernel<D, TERMS, MT, false, true>);
     else run(cache4_attn_kernel<D, TERMS, MT, false, false>);
   }
-  const int joins = p.nsplit > 1 ? p.rows : 0, chunks = keep ? (p.max_len + 4 * kThreads - 1) / (4 * kThreads) : 0;
+  const int slots = kThreads / (D / 4);
+  const int joins = p.nsplit == 1 ? 0 : p.nsplit <= kFewSplits ? (p.rows + slots - 1) / slots : p.rows;
+  const int chunks = keep ? (p.max_len + 4 * kThreads - 1) / (4 * kThreads) : 0;
   if (joins + chunks > 0)
     hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3(joins + chunks, p.Hkv, B), dim3(kThreads), 0, stream, p,
                        joins);
