@@ -674,13 +674,14 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   // Splits of whole steps of 128 keys. With one row tile memory is the bound: two
   // workgroups a CU, and splits of at most 512 keys, so that the CUs finish together
   // (32 samples of 10-16K rows: 512 keys 101 us, 1024 106 us, 2048 112 us, 4096 117
-  // us). With two the issue of instructions is: one workgroup a CU, since a split's
-  // start and end cost more than its keys and its part has to be joined (8 samples
-  // of 3200 rows, 5 queries: 256 workgroups 13.2 us, 512 14.3, 1664 19.5; 256 queries:
-  // 256 workgroups, no split, 48 us; 512 46 us and 12 us to join).
+  // us). With two the issue of instructions is, and a split's start and end cost more
+  // than its keys: one workgroup a CU at D = 128 (8 samples of 3200 rows, 5 queries:
+  // 256 workgroups 13.2 us, 512 14.3, 1664 19.5; 256 queries over 6528 rows with the
+  // join: 48.5, 49.7, 51.8 us at 256, 512, 768), two at D = 64, whose waves take half
+  // the registers (43.0, 36.8, 36.4 us).
   const int64_t groups = std::max<int64_t>(heads * lay.blocks, 1);
   const int64_t steps = std::max((max_len + kStep - 1) / kStep, 1);
-  const int64_t aim = per == 16 ? 512 : 256;  // workgroups
+  const int64_t aim = per == 16 || D == 64 ? 512 : 256;  // workgroups
   int64_t want = (aim + groups - 1) / groups;
   // at most 16384 workgroups: a part takes 4 * D bytes a row of the workspace
   if (per == 16) want = std::max(want, std::min<int64_t>((steps + 3) / 4, (16384 + groups - 1) / groups));
