@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kSelThreads) void cache4_select_kernel(EvictParams 
   if (want == 0) return;
 
   __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t s_digit, s_left;
+  __shared__ uint32_t s_digit, s_left, s_whole;
   __shared__ uint32_t s_wave[2][kSelWaves];
   const int tiles = (old + kTileKeys - 1) / kTileKeys;
   uint32_t key[KPT];
@@ -139,12 +139,18 @@ __global__ __launch_bounds__(kSelThreads) void cache4_select_kernel(EvictParams 
       const bool first = left <= above + h0;
       s_digit = first ? hi : hi - 1;
       s_left = left - (first ? above : above + h0);
+      s_whole = s_left == (first ? h0 : h1);
     }
     __syncthreads();
     prefix |= s_digit << shift;
     left = s_left;
+    if (s_whole) {  // every key with these bits is kept: no more of them are needed
+      prefix -= 1;  // no weight's key is 0
+      left = 0;
+      break;
+    }
   }
-  // prefix is the smallest key kept, `left` of its rows
+  // keys above prefix are kept, and `left` of those equal to it
   uint32_t done = 0, ties = 0;  // kept, and equal to it, in the tiles before
   for (int tile = 0; tile < tiles; ++tile) {
     if (tiles > 1) load(tile);
