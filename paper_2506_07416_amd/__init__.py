@@ -379,8 +379,9 @@ def cache4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_new:
     dev = cache.get_device()
     B, Hkv, cap, cptr = _cache_shape(cache, D)
     shape = (rows, Hkv, D)
+    # an empty tensor has no address; one that is never read stands in
     _enqueue("litevlm_cache4_append", dev, _float_code("k", k), B, Hkv, D, cap, max_new,
-             _arg("k", k, k.dtype, shape, dev), _arg("v", v, k.dtype, shape, dev),
+             _arg("k", k, k.dtype, shape, dev) or cptr, _arg("v", v, k.dtype, shape, dev) or cptr,
              _arg("cu_new", cu_new, torch.int32, (B + 1,), dev), _arg("start", start, torch.int32, (B,), dev), cptr,
              None if weight is None else _arg("weight", weight, torch.float32, (B, Hkv, cap), dev))
 
@@ -399,7 +400,7 @@ def cache4_read(cache: torch.Tensor, D: int, cu_rows: torch.Tensor, start: torch
     shape = (k.shape[0], Hkv, D)
     _enqueue("litevlm_cache4_read", dev, _float_code("k", k), B, Hkv, D, cap, max_rows, cptr,
              _arg("start", start, torch.int32, (B,), dev), _arg("cu_rows", cu_rows, torch.int32, (B + 1,), dev),
-             _arg("k", k, k.dtype, shape, dev), _arg("v", v, k.dtype, shape, dev))
+             _arg("k", k, k.dtype, shape, dev) or cptr, _arg("v", v, k.dtype, shape, dev) or cptr)
     return k, v
 
 
@@ -439,9 +440,9 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
         n = load().litevlm_cache4_attn_workspace(code, B, Hq, Hkv, D, max_q, max_len, weight_rows)
         workspace = torch.empty((n or 1,), dtype=torch.uint8, device=q.device)
     _enqueue("litevlm_cache4_attn", dev, code, B, Hq, Hkv, D, cap, max_q, max_len, weight_rows,
-             _arg("q", q, q.dtype, (rows, Hq, D), dev), _arg("cu_q", cu_q, torch.int32, (B + 1,), dev), cptr,
+             _arg("q", q, q.dtype, (rows, Hq, D), dev) or cptr, _arg("cu_q", cu_q, torch.int32, (B + 1,), dev), cptr,
              _arg("lengths", lengths, torch.int32, (B,), dev), softmax_scale,
-             _arg("out", out, q.dtype, (rows, Hq, D), dev), win, wout, _workspace(workspace, dev), workspace.nbytes)
+             _arg("out", out, q.dtype, (rows, Hq, D), dev) or cptr + 16, win, wout, _workspace(workspace, dev), workspace.nbytes)
     return out
 
 

@@ -117,8 +117,26 @@ def test_append_and_read_of_nothing():
     k = torch.zeros((0, 1, 64), device="cuda")
     lv.cache4_append(cache, torch.zeros((1, 1, 64), device="cuda"), torch.zeros((1, 1, 64), device="cuda"),
                      dev([0, 0, 0]), dev([0, 0]), 0)
-    torch.cuda.synchronize()
-    assert not cache.any() and k.numel() == 0
+    # no rows at all, though some may come
+    lv.cache4_append(cache, k, k, dev([0, 0, 0]), dev([3, 4]), 5)
+    kr, vr = lv.cache4_read(cache, 64, dev([0, 0, 0]), dev([3, 4]), 5, rows=0)
+    assert not cache.any() and kr.shape == vr.shape == (0, 1, 64)
+
+
+def test_attention_of_nothing():
+    """No queries: the weights pass through. No rows, or none that may be looked at: zeros."""
+    cache = torch.full((2, 2, 32 * 68), 255, dtype=torch.uint8, device="cuda")
+    w = torch.rand((2, 2, 32), device="cuda")
+    out = torch.full_like(w, 9.0)
+    q = torch.zeros((0, 4, 64), device="cuda")
+    o = lv.cache4_attn(cache, q, dev([0, 0, 0]), dev([3, 32]), 2, 32, weight=w, weight_out=out, weight_rows=1)
+    assert o.shape == q.shape and torch.equal(out[1], w[1]) and torch.equal(out[0, :, :3], w[0, :, :3])
+    assert (out[0, :, 3:] == 9).all()
+    q = torch.randn((3, 4, 64), device="cuda")
+    for lengths, max_len in (([0, 0], 32), ([5, 5], 0), ([-4, 0], 7)):
+        o = lv.cache4_attn(cache, q, dev([0, 1, 3]), dev(lengths), 2, max_len, weight=w, weight_out=out, weight_rows=2)
+        assert not o.any()
+    assert (out[0, :, 3:] == 9).all()
 
 
 # ----------------------------------------------------------------------------- attention
@@ -414,6 +432,19 @@ def test_verify_matches_oracle(case):
         assert int(got["n_accepted"][b]) == a, b
         assert got["tokens"][b].tolist() == tokens.tolist(), b
         assert int(got["lengths"][b]) == lengths[b] - (n[b] - a), b
+
+
+def test_verify_lengths_in_place():
+    """Without counts every draft counts; the cached lengths may be updated where they are."""
+    B, m, V = 4, 3, 50
+    p = torch.full((B, m + 1, V), 1 / V, device="cuda")
+    draft = torch.randint(0, V, (B, m), device="cuda").to(torch.int32)
+    u = torch.tensor([[0.0, 0.0, 0.0], [0.0, 0.9, 0.0], [0.9, 0.0, 0.0], [0.0, 0.0, 0.9]], device="cuda")
+    lengths = dev([10, 11, 12, 13])
+    r = lv.verify_draft(draft, p, None, u, torch.full((B,), 0.5, device="cuda"), lengths=lengths, out=dict(lengths=lengths))
+    # u < 1 / V accepts: 3, 1, 0 and 2 of 3 drafts
+    assert r["n_accepted"].tolist() == [3, 1, 0, 2]
+    assert lengths.tolist() == [10, 9, 9, 12] and r["lengths"] is lengths
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
