@@ -29,6 +29,7 @@ constexpr int kKeys = 32;              // keys of a wave's step
 constexpr int kStep = kWaves * kKeys;  // keys of a workgroup's step
 constexpr int kFewSplits = 4;          // splits of a row that one thread joins
 constexpr int kKept = 8;               // rows of a KV head whose logits are kept
+constexpr int kWhole = 512;            // keys up to which one workgroup takes them all
 constexpr float kSlack = 8.f;          // the running reference may lag the maximum by this (log2)
 
 struct AttnParams {
@@ -199,14 +200,21 @@ struct Attn {
   }
 };
 
+// What becomes of the logits of the rows that add weight.
+enum Keep {
+  kForget,    // no weights, or the logits are taken again
+  kWorkspace, // kept for the joining kernel
+  kLds        // all keys are this workgroup's: kept in LDS, it adds the weights itself
+};
+
 // One workgroup: 16 * MT rows of one (sample, KV head) and the keys of one split,
 // of which wave w takes steps of 32 keys w, w + 4, ... Each wave keeps its own
 // reference, sum and output; they are joined at the end. The reference of a row
 // follows its maximum only when a logit exceeds it by kSlack: until then the
 // probabilities are at most 2^kSlack, and neither an exchange between lanes nor a
 // rescaling of the output is needed.
-template <int D, int TERMS, int MT, bool KEEP, bool ONCE>
-__global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache4_attn_kernel(AttnParams p) {
+template <int D, int TERMS, int MT, Keep KEEP, bool ONCE>
+__global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? (KEEP == kLds ? 3 : 4) : 2) void cache4_attn_kernel(AttnParams p) {
   using A = Attn<D, TERMS>;
   constexpr int LD = D + 4;  // row of the joining buffer: 16 rows start in different banks
   __shared__ float s_o[kWaves][16 * LD];
@@ -217,12 +225,28 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
   const int b = blockIdx.y;
   const Sample sm(p, b);
   const int r0 = rb * 16 * MT;
-  if (r0 >= sm.rows) return;
+  const int64_t head = (int64_t)b * p.Hkv + g;
+  constexpr int kLogitRow = kWhole + 4;
+  __shared__ float s_logit[KEEP == kLds ? kKept * kLogitRow : 1];
+  __shared__ float2 s_stat[kKept];
+  // the weights from s_logit and s_stat, as the joining kernel takes them
+  const auto add_weights = [&](int rows) __attribute__((always_inline)) {
+    for (int k = tid; k < sm.n; k += kThreads) {
+      float w = 0.f;
+      for (int r = 0; r < rows; ++r)
+        w += k < sm.seen(p, r) ? __builtin_amdgcn_exp2f(s_logit[r * kLogitRow + k] - s_stat[r].x) * s_stat[r].y : 0.f;
+      const int64_t at = head * p.cap + k;
+      p.weight_out[at] = (p.weight_in ? p.weight_in[at] : 0.f) + w;
+    }
+  };
+  if (r0 >= sm.rows) {
+    if (KEEP == kLds) add_weights(0);  // no queries: the weights pass through
+    return;
+  }
   const int most = sm.seen(p, min(r0 + 16 * MT, sm.rows) - 1);  // keys that the block's last row sees
   const int begin = split * p.split_len, end = min(begin + p.split_len, most);
   if (begin >= end && split > 0) return;
   const int all = sm.seen(p, r0);  // keys that every row of the block sees
-  const int64_t head = (int64_t)b * p.Hkv + g;
   const CacheHead<D> c(p.cache, head, p.cap);
 
   typename A::Rows f[MT];
@@ -264,7 +288,12 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
     f32x4 s[2][MT];
     A::template logits<MT>(kc[0], f, s[0]);
     A::template logits<MT>(kc[1], f, s[1]);
-    if (KEEP) {
+    if (KEEP == kLds && col < p.wrows && col < kKept) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<f32x4*>(&s_logit[col * kLogitRow + k0 + 16 * h + 4 * lg]) = s[h][0] * p.scale_log2;
+    }
+    if (KEEP == kWorkspace) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         if (r0 + 16 * mt + col >= p.wrows) continue;
@@ -383,7 +412,8 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
         else static_cast<__bf16*>(p.o)[at + e] = (__bf16)z;
       }
       if (e0 == 0 && r < p.wrows) {
-        if (KEEP) p.part_ml[head * p.rows + r] = make_float2(top, all_l);
+        if (KEEP == kLds) s_stat[r] = make_float2(base, inv);
+        else if (KEEP == kWorkspace) p.part_ml[head * p.rows + r] = make_float2(top, all_l);
         else p.stat[head * p.wrows + r] = make_float2(base, inv);
       }
     } else {
@@ -392,6 +422,10 @@ __global__ __launch_bounds__(kThreads, TERMS == 1 && MT == 1 ? 4 : 2) void cache
       for (int e = 0; e < EPT; ++e) p.part_o[at * D + e0 + e] = y[e];
       if (e0 == 0) p.part_ml[at] = make_float2(top, all_l);
     }
+  }
+  if (KEEP == kLds) {
+    __syncthreads();
+    add_weights(min(sm.rows, p.wrows));
   }
 }
 
@@ -627,18 +661,23 @@ bool keep_logits(int wrows) { return wrows <= kKept; }
 template <int D, int TERMS, int MT>
 void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
   const bool weights = p.weight_rows > 0 && p.max_len > 0, keep = weights && keep_logits(p.wrows);
+  const bool whole = keep && p.nsplit == 1 && p.blocks == 1 && p.max_len <= kWhole;
   const dim3 grid(p.Hkv * p.blocks * p.nsplit, B);
   // keys of more caches than the last-level cache holds half of, each read by one
   // workgroup, pass it by (493 MB of 32 samples: 119 -> 113 us with the join; at
   // 3.7 MB, which stay in it, 4.6 -> 5.0 us)
   const bool once = p.blocks == 1 && CacheHead<D>::bytes(p.max_len) * p.Hkv * B > ((int64_t)128 << 20);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p); };
+  if (whole) {
+    run(cache4_attn_kernel<D, TERMS, MT, kLds, false>);
+    return;
+  }
   if (keep) {
-    if (once) run(cache4_attn_kernel<D, TERMS, MT, true, true>);
-    else run(cache4_attn_kernel<D, TERMS, MT, true, false>);
+    if (once) run(cache4_attn_kernel<D, TERMS, MT, kWorkspace, true>);
+    else run(cache4_attn_kernel<D, TERMS, MT, kWorkspace, false>);
   } else {
-    if (once) run(cache4_attn_kernel<D, TERMS, MT, false, true>);
-    else run(cache4_attn_kernel<D, TERMS, MT, false, false>);
+    if (once) run(cache4_attn_kernel<D, TERMS, MT, kForget, true>);
+    else run(cache4_attn_kernel<D, TERMS, MT, kForget, false>);
   }
   const int slots = kThreads / (D / 4);
   const int joins = p.nsplit == 1 ? 0 : p.nsplit <= kFewSplits ? (p.rows + slots - 1) / slots : p.rows;
@@ -647,7 +686,9 @@ void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
     hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3(joins + chunks, p.Hkv, B), dim3(kThreads), 0, stream, p,
                        joins);
   if (weights && !keep)
-    hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>), dim3((p.max_len + kWaves * kAgainKeys - 1) / (kWaves * kAgainKeys), p.Hkv, B), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>),
+                       dim3((p.max_len + kWaves * kAgainKeys - 1) / (kWaves * kAgainKeys), p.Hkv, B), dim3(kThreads), 0,
+                       stream, p);
 }
 
 template <int D>
@@ -686,6 +727,9 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   // at most 16384 workgroups: a part takes 4 * D bytes a row of the workspace
   if (per == 16) want = std::max(want, std::min<int64_t>((steps + 3) / 4, (16384 + groups - 1) / groups));
   want = std::min(want, steps);
+  // few keys: one workgroup a head, which adds the weights too, and one launch (8
+  // heads, 1 query, in a graph: 128 keys 4.4 us, 7.2 with a join; 512 keys 6.9 and 7.3)
+  if (max_len <= kWhole && lay.blocks == 1) want = 1;
   const int64_t each = (steps + want - 1) / want;
   lay.split_len = (int)(each * kStep);
   lay.nsplit = (int)((steps + each - 1) / each);

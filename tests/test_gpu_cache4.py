@@ -179,6 +179,9 @@ ATTN = [
     ([700, 701], [2, 1], 128, 1, 128, 704, "bf16", 2, 0),
     ([2500, 1300], [1, 1], 32, 8, 128, 2528, "bf16", 1, 28),
     ([2500], [70], 8, 2, 128, 2528, "bf16", 3, 0),
+    ([512, 1, 0, 77], [1, 2, 1, 0], 32, 8, 128, 512, "bf16", 2, 0),
+    ([512, 300], [2, 1], 16, 4, 64, 544, "f32", 2, 1),
+    ([513, 512], [7, 3], 16, 4, 128, 544, "bf16", 1, 0),
     ([1111, 900], [6, 1], 8, 4, 64, 1120, "f32", 6, 9),
 ]
 
