@@ -402,6 +402,11 @@ VERIFY = [
     (4, 64, 129, "f32", False),
     (7, 3, 4096, "bf16", True),
     (2, 5, 4097, "f32", True),
+    (5, 2, 8192, "f32", False),
+    (5, 2, 8193, "bf16", True),
+    (4, 3, 30001, "f32", True),
+    (4, 3, 32768, "bf16", False),
+    (4, 3, 32769, "f32", True),
     (6, 7, 50257, "bf16", True),
     (6, 2, 131072, "f32", True),
     (256, 2, 300, "f32", True),
@@ -451,7 +456,7 @@ def test_verify_lengths_in_place():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("V", [5, 9001])
+@pytest.mark.parametrize("V", [5, 9001, 40001])
 def test_verify_edges(dtype, V):
     """Ties and borders (all exact in 64 bits), empty rows, values that are no probabilities."""
     m = 2
