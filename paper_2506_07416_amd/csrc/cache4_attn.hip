@@ -649,8 +649,15 @@ __global__ __launch_bounds__(kThreads) void cache4_weight_again_kernel(AttnParam
 
 // Row tiles of a workgroup. Two decode a key once for 32 rows; four would hold 128
 // registers of outputs and leave one wave a SIMD (256 queries of 4 heads over 6528
-// rows: 2 tiles 46-48 us, 4 tiles 61 us, 1 tile 57 us).
-int row_tiles(int64_t rows) { return rows <= 16 ? 1 : 2; }
+// rows: 2 tiles 46-48 us, 4 tiles 61 us, 1 tile 57 us). While the steps of 16 rows and
+// 128 keys do not fill the chip, one tile in twice the workgroups is through sooner
+// (5 queries of 4 heads, on the GPU alone: 1500 rows 7.8 us and 9.0 with two tiles;
+// 1600 such steps 12.2 and 11.8 us, 3200 17.3 and 13.9), unless two save a launch.
+int row_tiles(int64_t rows, int64_t heads, int max_len) {
+  if (rows <= 16) return 1;
+  if (rows <= 32 && max_len <= kWhole) return 2;
+  return heads * ((rows + 15) / 16) * ((max_len + kStep - 1) / kStep) <= 1536 ? 1 : 2;
+}
 
 // Keeping the logits of a row costs 8 bytes a key (written and read), taking them
 // again D/2 + D/32 bytes a key for all of them, and a launch (8 samples of 3200 rows,
@@ -692,8 +699,7 @@ void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
 }
 
 template <int D>
-void launch_d(const AttnParams& p, int dtype, int B, hipStream_t stream) {
-  const int mt = row_tiles(p.rows);
+void launch_d(const AttnParams& p, int dtype, int B, int mt, hipStream_t stream) {
   if (dtype == LITEVLM_F32) {
     if (mt == 1) launch_mt<D, 3, 1>(p, B, stream);
     else launch_mt<D, 3, 2>(p, B, stream);
@@ -710,7 +716,8 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   Cache4AttnLayout lay;
   const int G = Hq / Hkv;
   const int64_t rows = (int64_t)max_q * G, wrows = (int64_t)weight_rows * G, heads = (int64_t)B * Hkv;
-  const int per = 16 * row_tiles(rows);
+  lay.tiles = row_tiles(rows, heads, max_len);
+  const int per = 16 * lay.tiles;
   lay.blocks = (int)((rows + per - 1) / per);
   // Splits of whole steps of 128 keys. With one row tile memory is the bound: two
   // workgroups a CU, and splits of at most 512 keys, so that the CUs finish together
@@ -777,8 +784,8 @@ hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream) {
   p.split_len = lay.split_len;
   p.lpad = lay.lpad;
   p.scale_log2 = a.scale_log2;
-  if (a.D == 128) launch_d<128>(p, a.dtype, a.B, stream);
-  else launch_d<64>(p, a.dtype, a.B, stream);
+  if (a.D == 128) launch_d<128>(p, a.dtype, a.B, lay.tiles, stream);
+  else launch_d<64>(p, a.dtype, a.B, lay.tiles, stream);
   return hipGetLastError();
 }
 

@@ -154,7 +154,7 @@ hipError_t launch_cache4_read(const Cache4RowsArgs& a, hipStream_t stream);
 //   stat     float2 [B][Hkv][weight rows]      (reference, 1 / sum) of the rows that add weight
 //   logit    float  [B][Hkv][weight rows][lpad] their logits, where they are kept
 struct Cache4AttnLayout {
-  int blocks, nsplit, split_len, lpad;
+  int tiles, blocks, nsplit, split_len, lpad;
   size_t part_o_off, part_ml_off, stat_off, logit_off, total;
 };
 Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, int max_q, int max_len,
