@@ -552,7 +552,7 @@ litevlm_status_t litevlm_cache4_read(int32_t dtype, int32_t B, int32_t Hkv, int3
                                      const int32_t* cu_rows, void* k, void* v, void* stream);
 
 /* Bytes of device workspace litevlm_cache4_attn needs for these sizes (0 when the
- * sizes are invalid). */
+ * sizes are invalid; 16 when it needs none and takes NULL). */
 size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
                                      int32_t max_q, int32_t max_len, int32_t weight_rows);
 
@@ -637,7 +637,8 @@ litevlm_status_t litevlm_cache4_evict(int32_t B, int32_t Hkv, int32_t D, int32_t
 /* Most drafted tokens of a sample that litevlm_verify_draft takes. */
 #define LITEVLM_MAX_DRAFT 64
 
-/* Bytes of device workspace litevlm_verify_draft needs (0 when the sizes are invalid). */
+/* Bytes of device workspace litevlm_verify_draft needs (0 when the sizes are invalid;
+ * 16 when it needs none and takes NULL). */
 size_t litevlm_verify_draft_workspace(int32_t B, int32_t max_draft, int32_t V);
 
 /*

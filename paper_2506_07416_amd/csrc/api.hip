@@ -540,6 +540,9 @@ litevlm_status_t check_cache4_rows(int32_t dtype, int32_t B, int32_t Hkv, int32_
   return LITEVLM_OK;
 }
 
+// What a workspace query answers for a call that needs none: 0 means invalid sizes.
+constexpr size_t kNoWorkspace = 16;
+
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
@@ -599,7 +602,7 @@ litevlm_status_t litevlm_cache4_read(int32_t dtype, int32_t B, int32_t Hkv, int3
 size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
                                      int32_t max_q, int32_t max_len, int32_t weight_rows) {
   if (check_cache4_attn(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows) != LITEVLM_OK) return 0;
-  return cache4_attn_layout(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows).total;
+  return std::max(cache4_attn_layout(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows).total, kNoWorkspace);
 }
 
 litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t cap,
@@ -622,7 +625,7 @@ litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32
   for (const void* p : small)
     if (p && !aligned(p, 4)) return LITEVLM_ERR_MISALIGNED;
   const size_t need = cache4_attn_layout(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows).total;
-  if (!workspace || workspace_bytes < need) return LITEVLM_ERR_WORKSPACE;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return LITEVLM_ERR_WORKSPACE;
   Cache4AttnArgs a;
   a.dtype = dtype;
   a.B = B;
@@ -702,7 +705,7 @@ static litevlm_status_t check_verify_shape(int32_t B, int32_t max_draft, int32_t
 
 size_t litevlm_verify_draft_workspace(int32_t B, int32_t max_draft, int32_t V) {
   if (check_verify_shape(B, max_draft, V) != LITEVLM_OK) return 0;
-  return verify_layout(B, V).total;
+  return std::max(verify_layout(B, V).total, kNoWorkspace);
 }
 
 litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draft, int32_t V,
@@ -722,7 +725,8 @@ litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draf
   const void* small[] = {draft, n_draft, u, r, lengths, tokens, n_accepted, lengths_out};
   for (const void* p : small)
     if (p && !aligned(p, 4)) return LITEVLM_ERR_MISALIGNED;
-  if (!workspace || workspace_bytes < verify_layout(B, V).total) return LITEVLM_ERR_WORKSPACE;
+  const size_t need = verify_layout(B, V).total;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return LITEVLM_ERR_WORKSPACE;
   VerifyArgs a;
   a.dtype = dtype;
   a.B = B;

@@ -663,19 +663,18 @@ int row_tiles(int64_t rows, int64_t heads, int max_len) {
 // again D/2 + D/32 bytes a key for all of them, and a launch (8 samples of 3200 rows,
 // the whole call: 4 rows 16.1 us kept, 24.1 again; 8 rows 18.7 and 23.8; 12 rows
 // 30.1 and 23.9; 4 samples of 16300 rows: 8 rows 28.4 and 43.6, 12 rows 53 and 42).
-bool keep_logits(int wrows) { return wrows <= kKept; }
+bool keep_logits(int64_t wrows) { return wrows <= kKept; }
 
 template <int D, int TERMS, int MT>
-void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
-  const bool weights = p.weight_rows > 0 && p.max_len > 0, keep = weights && keep_logits(p.wrows);
-  const bool whole = keep && p.nsplit == 1 && p.blocks == 1 && p.max_len <= kWhole;
+void launch_mt(const AttnParams& p, int B, const Cache4AttnLayout& lay, hipStream_t stream) {
+  const bool keep = lay.keep;
   const dim3 grid(p.Hkv * p.blocks * p.nsplit, B);
   // keys of more caches than the last-level cache holds half of, each read by one
   // workgroup, pass it by (493 MB of 32 samples: 119 -> 113 us with the join; at
   // 3.7 MB, which stay in it, 4.6 -> 5.0 us)
   const bool once = p.blocks == 1 && CacheHead<D>::bytes(p.max_len) * p.Hkv * B > ((int64_t)128 << 20);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p); };
-  if (whole) {
+  if (lay.whole) {
     run(cache4_attn_kernel<D, TERMS, MT, kLds, false>);
     return;
   }
@@ -692,20 +691,20 @@ void launch_mt(const AttnParams& p, int B, hipStream_t stream) {
   if (joins + chunks > 0)
     hipLaunchKernelGGL((cache4_join_kernel<D, TERMS, MT>), dim3(joins + chunks, p.Hkv, B), dim3(kThreads), 0, stream, p,
                        joins);
-  if (weights && !keep)
+  if (p.wrows > 0 && !keep)
     hipLaunchKernelGGL((cache4_weight_again_kernel<D, TERMS>),
                        dim3((p.max_len + kWaves * kAgainKeys - 1) / (kWaves * kAgainKeys), p.Hkv, B), dim3(kThreads), 0,
                        stream, p);
 }
 
 template <int D>
-void launch_d(const AttnParams& p, int dtype, int B, int mt, hipStream_t stream) {
+void launch_d(const AttnParams& p, int dtype, int B, const Cache4AttnLayout& lay, hipStream_t stream) {
   if (dtype == LITEVLM_F32) {
-    if (mt == 1) launch_mt<D, 3, 1>(p, B, stream);
-    else launch_mt<D, 3, 2>(p, B, stream);
+    if (lay.tiles == 1) launch_mt<D, 3, 1>(p, B, lay, stream);
+    else launch_mt<D, 3, 2>(p, B, lay, stream);
   } else {
-    if (mt == 1) launch_mt<D, 1, 1>(p, B, stream);
-    else launch_mt<D, 1, 2>(p, B, stream);
+    if (lay.tiles == 1) launch_mt<D, 1, 1>(p, B, lay, stream);
+    else launch_mt<D, 1, 2>(p, B, lay, stream);
   }
 }
 
@@ -741,15 +740,17 @@ Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, in
   lay.split_len = (int)(each * kStep);
   lay.nsplit = (int)((steps + each - 1) / each);
   lay.lpad = (max_len + kKeys - 1) / kKeys * kKeys;
+  const bool weights = weight_rows > 0 && max_len > 0;
+  lay.keep = weights && keep_logits(wrows);
+  lay.whole = lay.keep && lay.nsplit == 1 && lay.blocks == 1 && max_len <= kWhole;
   const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  const bool keep = keep_logits((int)wrows);
+  const bool logits = lay.keep && !lay.whole;
   const size_t parts = (size_t)heads * rows * lay.nsplit;
   lay.part_o_off = 0;
   lay.part_ml_off = up(lay.nsplit > 1 ? parts * D * sizeof(float) : 0);
-  lay.stat_off = lay.part_ml_off + up(lay.nsplit > 1 || keep ? parts * sizeof(float2) : 0);
-  lay.logit_off = lay.stat_off + up((size_t)heads * wrows * sizeof(float2));
-  lay.total = lay.logit_off + up(keep ? (size_t)heads * wrows * lay.lpad * sizeof(float) : 0);
-  lay.total = std::max<size_t>(lay.total, 256);
+  lay.stat_off = lay.part_ml_off + up(lay.nsplit > 1 || logits ? parts * sizeof(float2) : 0);
+  lay.logit_off = lay.stat_off + up(weights && !lay.whole ? (size_t)heads * wrows * sizeof(float2) : 0);
+  lay.total = lay.logit_off + up(logits ? (size_t)heads * wrows * lay.lpad * sizeof(float) : 0);
   return lay;
 }
 
@@ -778,14 +779,14 @@ hipError_t launch_cache4_attn(const Cache4AttnArgs& a, hipStream_t stream) {
   p.max_len = a.max_len;
   p.weight_rows = a.weight_rows;
   p.rows = a.max_q * p.G;
-  p.wrows = a.weight_rows * p.G;
+  p.wrows = a.max_len > 0 ? a.weight_rows * p.G : 0;
   p.blocks = lay.blocks;
   p.nsplit = lay.nsplit;
   p.split_len = lay.split_len;
   p.lpad = lay.lpad;
   p.scale_log2 = a.scale_log2;
-  if (a.D == 128) launch_d<128>(p, a.dtype, a.B, lay.tiles, stream);
-  else launch_d<64>(p, a.dtype, a.B, lay.tiles, stream);
+  if (a.D == 128) launch_d<128>(p, a.dtype, a.B, lay, stream);
+  else launch_d<64>(p, a.dtype, a.B, lay, stream);
   return hipGetLastError();
 }
 

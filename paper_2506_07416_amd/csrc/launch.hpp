@@ -153,8 +153,10 @@ hipError_t launch_cache4_read(const Cache4RowsArgs& a, hipStream_t stream);
 //   part_ml  float2 [B][Hkv][rows][nsplit]     their (reference, sum)
 //   stat     float2 [B][Hkv][weight rows]      (reference, 1 / sum) of the rows that add weight
 //   logit    float  [B][Hkv][weight rows][lpad] their logits, where they are kept
+// Each part may be missing; a call that takes one launch has none (total 0).
 struct Cache4AttnLayout {
   int tiles, blocks, nsplit, split_len, lpad;
+  bool keep, whole;  // logits kept; and the weights added by the first kernel
   size_t part_o_off, part_ml_off, stat_off, logit_off, total;
 };
 Cache4AttnLayout cache4_attn_layout(int dtype, int B, int Hq, int Hkv, int D, int max_q, int max_len,
@@ -187,8 +189,10 @@ struct Cache4EvictArgs {
 hipError_t launch_cache4_evict(const Cache4EvictArgs& a, hipStream_t stream);
 
 // Workspace of the draft verification: per (sample, chunk of the vocabulary) two
-// sums in 64 bits, and per sample the accepted drafts.
+// sums in 64 bits, and per sample the accepted drafts; nothing (total 0) where one
+// workgroup takes a sample.
 struct VerifyLayout {
+  bool one;
   int chunks;
   size_t acc_off, total;
 };

@@ -386,11 +386,11 @@ __global__ __launch_bounds__(kOneThreads) void verify_one_kernel(VerifyParams p)
 }
 
 template <bool BF16>
-void launch(const VerifyParams& p, int B, hipStream_t stream) {
-  // One launch while a workgroup keeps up: 2.3 us less for the host that launches
-  // (13.2 -> 11 us a pass), on the GPU alone, in a graph, 5.3, 6.2, 7.0 and 8.1 us for 1
+void launch(const VerifyParams& p, int B, bool one, hipStream_t stream) {
+  // One launch while a workgroup keeps up: 2.3 us less for the host that launches and
+  // 2.4 for a workspace that is not needed (13.2 -> 8.9 us a pass), on the GPU alone, in a graph, 5.3, 6.2, 7.0 and 8.1 us for 1
   // to 4 tiles against 6.4 for two launches.
-  if (p.V <= kOneTiles * kOneTile) {
+  if (one) {
     hipLaunchKernelGGL(verify_one_kernel<BF16>, dim3(B), dim3(kOneThreads), 0, stream, p);
   } else {
     hipLaunchKernelGGL(verify_sum_kernel<BF16>, dim3(p.chunks, B), dim3(kThreads), 0, stream, p);
@@ -404,7 +404,8 @@ VerifyLayout verify_layout(int B, int V) {
   VerifyLayout lay;
   lay.chunks = (V + kChunk - 1) / kChunk;
   lay.acc_off = (size_t)B * lay.chunks * sizeof(double2);
-  lay.total = lay.acc_off + (size_t)B * sizeof(Accepted);
+  lay.one = V <= kOneTiles * kOneTile;
+  lay.total = lay.one ? 0 : lay.acc_off + (size_t)B * sizeof(Accepted);
   return lay;
 }
 
@@ -427,8 +428,8 @@ hipError_t launch_verify_draft(const VerifyArgs& a, hipStream_t stream) {
   p.m = a.max_draft;
   p.V = a.V;
   p.chunks = lay.chunks;
-  if (a.dtype == LITEVLM_BF16) launch<true>(p, a.B, stream);
-  else launch<false>(p, a.B, stream);
+  if (a.dtype == LITEVLM_BF16) launch<true>(p, a.B, lay.one, stream);
+  else launch<false>(p, a.B, lay.one, stream);
   return hipGetLastError();
 }
 

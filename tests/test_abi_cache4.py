@@ -82,9 +82,13 @@ def test_attn_refusals():
         assert attn(**{name: A + 8}) == _abi.ERR_MISALIGNED
     for name in ("cu", "ln", "wi", "wo"):
         assert attn(**{name: A + 2}) == _abi.ERR_MISALIGNED
-    assert attn(ws=None) == _abi.ERR_WORKSPACE
-    assert attn(wsb=1) == _abi.ERR_WORKSPACE
+    big = dict(cap=2048, ml=2048)             # small calls need no workspace
+    assert attn(ws=None, **big) == _abi.ERR_WORKSPACE
+    assert attn(wsb=1, **big) == _abi.ERR_WORKSPACE
     lib = lv.load()
+    assert lib.litevlm_cache4_attn_workspace(_abi.BF16, 2, 8, 2, 128, 4, 2048, 1) > 16
+    assert lib.litevlm_cache4_attn_workspace(_abi.BF16, 2, 8, 2, 128, 4, 512, 1) == 16
+    assert lib.litevlm_cache4_attn_workspace(_abi.BF16, 2, 8, 2, 128, 4, 512, 4) > 16
     assert lib.litevlm_cache4_attn_workspace(_abi.BF16, 2, 8, 2, 128, 4, 64, 1) > 0
     assert lib.litevlm_cache4_attn_workspace(_abi.BF16, 2, 8, 3, 128, 4, 64, 1) == 0
     assert lib.litevlm_cache4_attn_workspace(_abi.BF16, 2, 8, 2, 128, 4, 64, 5) == 0
@@ -116,7 +120,7 @@ def test_evict_refusals():
     assert evict(ki=at(4)) == _abi.ERR_BAD_VALUE
 
 
-def verify(dt=_abi.F32, B=2, m=3, V=100, draft=at(0), nd=at(1), p=at(2), q=at(3), u=at(4), r=at(5), ln=at(6), tk=at(7),
+def verify(dt=_abi.F32, B=2, m=3, V=40000, draft=at(0), nd=at(1), p=at(2), q=at(3), u=at(4), r=at(5), ln=at(6), tk=at(7),
            na=at(8), lo=at(9), ws=at(10), wsb=None):
     lib = lv.load()
     if wsb is None:
@@ -136,6 +140,8 @@ def test_verify_refusals():
         assert verify(**{name: A + 2}) == _abi.ERR_MISALIGNED
     assert verify(ws=None) == _abi.ERR_WORKSPACE
     assert verify(wsb=0) == _abi.ERR_WORKSPACE
+    assert lv.load().litevlm_verify_draft_workspace(2, 3, 32768) == 16    # a small vocabulary needs none
+    assert lv.load().litevlm_verify_draft_workspace(2, 3, 32769) > 16
     assert verify(nd=None, q=None, ln=None, lo=None, ws=None) == _abi.ERR_WORKSPACE   # optional arguments
 
 
