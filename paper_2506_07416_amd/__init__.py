@@ -358,15 +358,15 @@ def _workspace(t: Optional[torch.Tensor], dev: int) -> tuple:
     return t.data_ptr(), t.nbytes
 
 
-def _cache_shape(cache: torch.Tensor, D: int):
-    """(B, Hkv, cap) of a cache tensor of head dim D, and its address."""
+def _cache_shape(cache: torch.Tensor, D: int, dev: int):
+    """(B, Hkv, cap) of a cache tensor of head dim D on device `dev`, and its address."""
     if D not in (64, 128):
         raise ValueError(f"head dim {D}: 64 or 128 expected")
     B, Hkv, n = cache.shape
     cap, rest = divmod(n, D + D // 16)
     if rest:
         raise ValueError(f"a cache of head dim {D} has {D + D // 16} bytes a position, not {n} for all of them")
-    return B, Hkv, cap, _arg("cache", cache, torch.uint8, (B, Hkv, n), cache.get_device())
+    return B, Hkv, cap, _arg("cache", cache, torch.uint8, (B, Hkv, n), dev)
 
 
 def cache4_empty(B: int, Hkv: int, D: int, cap: int, device="cuda") -> torch.Tensor:
@@ -385,7 +385,7 @@ def cache4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_new:
     0 at those positions."""
     rows, _, D = k.shape
     dev = cache.get_device()
-    B, Hkv, cap, cptr = _cache_shape(cache, D)
+    B, Hkv, cap, cptr = _cache_shape(cache, D, dev)
     shape = (rows, Hkv, D)
     # an empty tensor has no address; one that is never read stands in
     _enqueue("litevlm_cache4_append", dev, _float_code("k", k), B, Hkv, D, cap, max_new,
@@ -399,8 +399,8 @@ def cache4_read(cache: torch.Tensor, D: int, cu_rows: torch.Tensor, start: torch
     """The values of cached rows: rows cu_rows[b].. of the packed result are positions start[b]..
     of sample b. Returns (k, v) [rows,Hkv,D]; without `out` they have `rows` rows (B * max_rows by
     default) of `dtype`, and rows past cu_rows[B] are not written."""
-    B, Hkv, cap, cptr = _cache_shape(cache, D)
     dev = cache.get_device()
+    B, Hkv, cap, cptr = _cache_shape(cache, D, dev)
     if out is None:
         shape = (B * max_rows if rows is None else rows, Hkv, D)
         out = (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
@@ -428,7 +428,7 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
     Returns [rows,Hq,D] in q's type."""
     rows, Hq, D = q.shape
     dev = cache.get_device()
-    B, Hkv, cap, cptr = _cache_shape(cache, D)
+    B, Hkv, cap, cptr = _cache_shape(cache, D, dev)
     code = _float_code("q", q)
     if softmax_scale is None:
         softmax_scale = 1.0 / math.sqrt(D)
@@ -461,12 +461,12 @@ def cache4_evict(cache: torch.Tensor, D: int, weight: torch.Tensor, lengths: tor
     largest weight [B,Hkv,cap]. Returns a dict of new tensors: cache (of cap_out positions, by
     default budget rounded up to 32), weight [B,Hkv,cap_out], lengths [B] and kept_index
     [B,Hkv,budget], all valid up to lengths[b]. ``out`` may supply them under the same keys."""
-    B, Hkv, cap, cptr = _cache_shape(cache, D)
     dev, device = cache.get_device(), cache.device
+    B, Hkv, cap, cptr = _cache_shape(cache, D, dev)
     o = dict(out or {})
     if "cache" not in o:
         o["cache"] = cache4_empty(B, Hkv, D, (budget + 31) // 32 * 32 if cap_out is None else cap_out, device)
-    B2, H2, cap_out, optr = _cache_shape(o["cache"], D)
+    B2, H2, cap_out, optr = _cache_shape(o["cache"], D, dev)
     if (B2, H2) != (B, Hkv):
         raise ValueError(f"the new cache is for {B2} samples and {H2} heads, not {B} and {Hkv}")
     if "weight" not in o:
