@@ -626,7 +626,7 @@ litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32
  *   kept_index         dev out int32 [B, Hkv, budget]: each kept row's former position,
  *                      ascending; entries past lengths_out[b] are untouched, as are the
  *                      new cache's rows and weights there
- * No output may overlap an input (LITEVLM_ERR_BAD_VALUE).
+ * No output may overlap an input or another output (LITEVLM_ERR_BAD_VALUE).
  */
 litevlm_status_t litevlm_cache4_evict(int32_t B, int32_t Hkv, int32_t D, int32_t cap, int32_t cap_out,
                                       int32_t max_len, int32_t budget, int32_t recent, const void* cache,
@@ -677,7 +677,8 @@ size_t litevlm_verify_draft_workspace(int32_t B, int32_t max_draft, int32_t V);
  *                      lengths[b] - (n - a), the rows that stay valid
  *   workspace          dev scratch of litevlm_verify_draft_workspace() bytes (contents on
  *                      entry ignored; calls that may run concurrently must not share one)
- * Except for lengths_out, no output may overlap an input.
+ * No output and no workspace may overlap an input or another output, but lengths_out
+ * may be lengths (LITEVLM_ERR_BAD_VALUE).
  */
 litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draft, int32_t V,
                                       const int32_t* draft, const int32_t* n_draft, const void* target,

@@ -543,9 +543,28 @@ litevlm_status_t check_cache4_rows(int32_t dtype, int32_t B, int32_t Hkv, int32_
 // What a workspace query answers for a call that needs none: 0 means invalid sizes.
 constexpr size_t kNoWorkspace = 16;
 
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
+// A buffer of a call; no address, or no bytes, where it is not used.
+struct Span {
+  const void* p;
+  size_t n;
+};
+
+bool overlap(const Span& a, const Span& b) {
+  if (!a.p || !b.p || a.n == 0 || b.n == 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x < y + b.n && y < x + a.n;
+}
+
+// Whether an output shares memory with an input or with another output.
+template <int NI, int NO>
+bool overlap(const Span (&in)[NI], const Span (&out)[NO]) {
+  for (int i = 0; i < NO; ++i) {
+    for (const Span& x : in)
+      if (overlap(x, out[i])) return true;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[j], out[i])) return true;
+  }
+  return false;
 }
 
 }  // namespace
@@ -664,20 +683,12 @@ litevlm_status_t litevlm_cache4_evict(int32_t B, int32_t Hkv, int32_t D, int32_t
       !aligned(lengths, 4) || !aligned(lengths_out, 4) || !aligned(kept_index, 4))
     return LITEVLM_ERR_MISALIGNED;
   const size_t heads = (size_t)B * Hkv;
-  const struct {
-    const void* p;
-    size_t n;
-  } in[] = {{cache, litevlm_cache4_bytes(B, Hkv, D, cap)}, {weight, heads * cap * 4}, {lengths, (size_t)B * 4}},
-    out[] = {{cache_out, litevlm_cache4_bytes(B, Hkv, D, cap_out)},
-             {weight_out, heads * cap_out * 4},
-             {lengths_out, (size_t)B * 4},
-             {kept_index, heads * budget * 4}};
-  for (int i = 0; i < 4; ++i) {
-    for (const auto& x : in)
-      if (overlap(x.p, x.n, out[i].p, out[i].n)) return LITEVLM_ERR_BAD_VALUE;
-    for (int j = 0; j < i; ++j)
-      if (overlap(out[j].p, out[j].n, out[i].p, out[i].n)) return LITEVLM_ERR_BAD_VALUE;
-  }
+  const Span in[] = {{cache, litevlm_cache4_bytes(B, Hkv, D, cap)}, {weight, heads * cap * 4}, {lengths, (size_t)B * 4}};
+  const Span out[] = {{cache_out, litevlm_cache4_bytes(B, Hkv, D, cap_out)},
+                      {weight_out, heads * cap_out * 4},
+                      {lengths_out, (size_t)B * 4},
+                      {kept_index, heads * budget * 4}};
+  if (overlap(in, out)) return LITEVLM_ERR_BAD_VALUE;
   Cache4EvictArgs a;
   a.B = B;
   a.Hkv = Hkv;
@@ -725,7 +736,13 @@ litevlm_status_t litevlm_verify_draft(int32_t dtype, int32_t B, int32_t max_draf
   const void* small[] = {draft, n_draft, u, r, lengths, tokens, n_accepted, lengths_out};
   for (const void* p : small)
     if (p && !aligned(p, 4)) return LITEVLM_ERR_MISALIGNED;
-  const size_t need = verify_layout(B, V).total;
+  const size_t need = verify_layout(B, V).total, n = (size_t)B * 4, drafts = n * max_draft;
+  const size_t row = (size_t)V * (dtype == LITEVLM_F32 ? 4 : 2);
+  const Span in[] = {{draft, drafts}, {n_draft, n}, {target, B * (max_draft + 1) * row}, {proposal, B * max_draft * row},
+                     {u, drafts}, {r, n}, {lengths == lengths_out ? nullptr : lengths, n}};
+  const Span out[] = {{tokens, drafts + n}, {n_accepted, n}, {lengths ? lengths_out : nullptr, n},
+                      {workspace, workspace_bytes < need ? 0 : need}};
+  if (overlap(in, out)) return LITEVLM_ERR_BAD_VALUE;
   if (need > 0 && (!workspace || workspace_bytes < need)) return LITEVLM_ERR_WORKSPACE;
   VerifyArgs a;
   a.dtype = dtype;

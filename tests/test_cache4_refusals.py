@@ -49,3 +49,51 @@ def test_evict_refuses_a_new_cache_elsewhere(calls):
             with pytest.raises(ValueError, match="device"):
                 lv.cache4_evict(*evict_args(), 20, 4, 64, out=out)
     assert len(calls) == 1
+
+
+# ----------------------------------------------------------------------------- buffers that overlap
+
+def at(i):
+    """Fake buffers far apart: the library's checks read none of them."""
+    return 0x7F0000000000 + (i << 36)
+
+
+VERIFY_IN = dict(draft=at(0), nd=at(1), p=at(2), q=at(3), u=at(4), r=at(5), ln=at(6))
+VERIFY_OUT = dict(tk=at(7), na=at(8), lo=at(9))
+
+
+def verify(B=3, m=4, V=40000, dt=lv._abi.F32, ws=at(10), wsb=0, **a):
+    a = {**VERIFY_IN, **VERIFY_OUT, **a}
+    # too small a workspace: a call whose buffers are accepted ends there, on the host
+    return lv.load().litevlm_verify_draft(dt, B, m, V, a["draft"], a["nd"], a["p"], a["q"], a["u"], a["r"], a["ln"], a["tk"],
+                                          a["na"], a["lo"], ws, wsb, None)
+
+
+def test_verify_refuses_outputs_over_inputs_and_each_other():
+    B, m, V = 3, 4, 40000
+    bad, fine = lv._abi.ERR_BAD_VALUE, lv._abi.ERR_WORKSPACE
+    size = dict(draft=B * m, nd=B, p=B * (m + 1) * V, q=B * m * V, u=B * m, r=B, ln=B, tk=B * (m + 1), na=B, lo=B)
+    assert verify() == fine
+    for out in VERIFY_OUT:
+        for other in list(VERIFY_IN) + list(VERIFY_OUT):
+            if other == out:
+                continue
+            base = {**VERIFY_IN, **VERIFY_OUT}[other]
+            n, own = 4 * size[other], 4 * size[out]
+            same = fine if (out, other) in (("lo", "ln"), ("ln", "lo")) else bad
+            assert verify(**{out: base}) == same, (out, other)
+            for off in (4 - own, n - 4) if own > 4 else (n - 4,):
+                if off:
+                    assert verify(**{out: base + off}) == bad, (out, other, off)
+            assert verify(**{out: base + n}) == fine and verify(**{out: base - own}) == fine, (out, other)
+    half = dict(dt=lv._abi.BF16)              # two bytes a probability
+    assert verify(**half, tk=at(2) + 2 * size["p"]) == fine and verify(**half, tk=at(2) + 2 * size["p"] - 4) == bad
+    # what is not given is not looked at
+    assert verify(nd=None, q=None, ln=None, lo=at(7)) == fine
+
+
+def test_verify_refuses_a_workspace_over_its_buffers():
+    wsb = lv.verify_draft_workspace_bytes(3, 4, 40000)
+    for name in list(VERIFY_IN) + list(VERIFY_OUT):
+        base = {**VERIFY_IN, **VERIFY_OUT}[name]
+        assert verify(ws=base, wsb=wsb) == lv._abi.ERR_BAD_VALUE, name
