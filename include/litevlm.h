@@ -586,13 +586,16 @@ size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32
  *   cu_q               dev int32 [B+1], non-decreasing, cu_q[0] = 0
  *   lengths            dev int32 [B]
  *   softmax_scale      finite, > 0
- *   o                  dev out [total, Hq, D], not over q; rows past total are untouched
+ *   o                  dev out [total, Hq, D]; rows past total are untouched
  *   weight_in          dev fp32 [B, Hkv, cap], or NULL = 0 (ignored when weight_rows is 0)
  *   weight_out         dev out fp32 [B, Hkv, cap], required when weight_rows > 0 (may be
  *                      weight_in): written for j < n_b, untouched behind
  *   workspace          dev scratch of litevlm_cache4_attn_workspace() bytes; contents on
  *                      entry are ignored, and calls that may run concurrently must not
  *                      share one
+ * No output and no workspace may overlap an input or another output, but weight_out may
+ * be weight_in (LITEVLM_ERR_BAD_VALUE; of q and o, whose rows only the device knows,
+ * the library sees only o == q).
  */
 litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t cap,
                                      int32_t max_q, int32_t max_len, int32_t weight_rows, const void* q,

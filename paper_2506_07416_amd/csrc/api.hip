@@ -644,6 +644,11 @@ litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32
   for (const void* p : small)
     if (p && !aligned(p, 4)) return LITEVLM_ERR_MISALIGNED;
   const size_t need = cache4_attn_layout(dtype, B, Hq, Hkv, D, max_q, max_len, weight_rows).total;
+  const size_t nw = weight_rows > 0 ? (size_t)B * Hkv * cap * 4 : 0;
+  const Span in[] = {{cache, litevlm_cache4_bytes(B, Hkv, D, cap)}, {cu_q, (size_t)(B + 1) * 4}, {lengths, (size_t)B * 4},
+                     {weight_in == weight_out ? nullptr : weight_in, nw}};
+  const Span out[] = {{weight_out, nw}, {workspace, workspace_bytes < need ? 0 : need}};
+  if (overlap(in, out)) return LITEVLM_ERR_BAD_VALUE;
   if (need > 0 && (!workspace || workspace_bytes < need)) return LITEVLM_ERR_WORKSPACE;
   Cache4AttnArgs a;
   a.dtype = dtype;

@@ -97,3 +97,24 @@ def test_verify_refuses_a_workspace_over_its_buffers():
     for name in list(VERIFY_IN) + list(VERIFY_OUT):
         base = {**VERIFY_IN, **VERIFY_OUT}[name]
         assert verify(ws=base, wsb=wsb) == lv._abi.ERR_BAD_VALUE, name
+
+
+def attn(dt=lv._abi.BF16, B=2, Hq=8, H=2, D=128, cap=2048, mq=4, ml=2048, wr=1, q=at(0), cu=at(1), cache=at(2), ln=at(3),
+         scale=0.1, o=at(4), wi=at(5), wo=at(6), ws=at(7), wsb=0):
+    return lv.load().litevlm_cache4_attn(dt, B, Hq, H, D, cap, mq, ml, wr, q, cu, cache, ln, scale, o, wi, wo, ws, wsb, None)
+
+
+def test_attention_refuses_weights_over_its_inputs():
+    bad, fine = lv._abi.ERR_BAD_VALUE, lv._abi.ERR_WORKSPACE
+    n = 2 * 2 * 2048 * 4
+    assert attn() == fine and attn(wi=at(6)) == fine            # in place
+    for off in (4, -4, n - 4, 4 - n):
+        assert attn(wo=at(5) + off) == bad, off
+    assert attn(wo=at(5) + n) == fine and attn(wo=at(5) - n) == fine
+    assert attn(wo=at(2)) == bad and attn(wo=at(2) + 4 * 2048 * 136 - 4) == bad and attn(wo=at(2) + 4 * 2048 * 136) == fine
+    assert attn(wo=at(1) + 8) == bad and attn(wo=at(1) + 12) == fine and attn(wo=at(3) + 4) == bad
+    # without weights neither address counts
+    assert attn(wr=0, wo=at(5) + 4) == fine and attn(wr=0, wo=at(2)) == fine
+    wsb = lv.cache4_attn_workspace_bytes(torch.bfloat16, 2, 8, 2, 128, 4, 2048, 1)
+    for at_ws in (at(2), at(5), at(6), at(1) - 16, at(3) - wsb + 16):
+        assert attn(ws=at_ws, wsb=wsb) == bad
