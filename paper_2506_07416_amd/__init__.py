@@ -358,6 +358,11 @@ def _workspace(t: Optional[torch.Tensor], dev: int) -> tuple:
     return t.data_ptr(), t.nbytes
 
 
+def _overlap(a: int, na: int, b: int, nb: int) -> bool:
+    """Whether na bytes at a and nb bytes at b, both some, share any."""
+    return a < b + nb and b < a + na
+
+
 def _cache_shape(cache: torch.Tensor, D: int, dev: int):
     """(B, Hkv, cap) of a cache tensor of head dim D on device `dev`, and its address."""
     if D not in (64, 128):
@@ -432,8 +437,10 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
     code = _float_code("q", q)
     if softmax_scale is None:
         softmax_scale = 1.0 / math.sqrt(D)
-    if out is None:
+    fresh = out is None
+    if fresh:
         out = torch.empty_like(q)
+    qptr, optr = _arg("q", q, q.dtype, (rows, Hq, D), dev), _arg("out", out, q.dtype, (rows, Hq, D), dev)
     win = wout = None
     if weight_rows:
         if weight is not None:
@@ -444,14 +451,19 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
             wout = win
         else:
             wout = _arg("weight_out", weight_out, torch.float32, (B, Hkv, cap), dev)
+    if rows and not fresh:
+        n, nw = rows * Hq * D * (4 if code == _abi.F32 else 2), B * Hkv * cap * 4
+        if (_overlap(optr, n, qptr, n) or _overlap(optr, n, cptr, cache.nbytes)
+                or wout is not None and (_overlap(optr, n, wout, nw) or win is not None and _overlap(optr, n, win, nw))):
+            raise ValueError("out: overlaps q, the cache or a weight")
     if workspace is None:
         n = load().litevlm_cache4_attn_workspace(code, B, Hq, Hkv, D, max_q, max_len, weight_rows)
         if n > _NO_WORKSPACE:
             workspace = torch.empty((n,), dtype=torch.uint8, device=q.device)
     _enqueue("litevlm_cache4_attn", dev, code, B, Hq, Hkv, D, cap, max_q, max_len, weight_rows,
-             _arg("q", q, q.dtype, (rows, Hq, D), dev) or cptr, _arg("cu_q", cu_q, torch.int32, (B + 1,), dev), cptr,
-             _arg("lengths", lengths, torch.int32, (B,), dev), softmax_scale,
-             _arg("out", out, q.dtype, (rows, Hq, D), dev) or cptr + 16, win, wout, *_workspace(workspace, dev))
+             qptr or cptr, _arg("cu_q", cu_q, torch.int32, (B + 1,), dev), cptr,
+             _arg("lengths", lengths, torch.int32, (B,), dev), softmax_scale, optr or cptr + 16, win, wout,
+             *_workspace(workspace, dev))
     return out
 
 

@@ -118,3 +118,41 @@ def test_attention_refuses_weights_over_its_inputs():
     wsb = lv.cache4_attn_workspace_bytes(torch.bfloat16, 2, 8, 2, 128, 4, 2048, 1)
     for at_ws in (at(2), at(5), at(6), at(1) - 16, at(3) - wsb + 16):
         assert attn(ws=at_ws, wsb=wsb) == bad
+
+
+# ----------------------------------------------------------------------------- the same in the binding
+
+def attn_args(rows=5, Hq=4, D=64, B=2, H=2, cap=64, q=None):
+    cache = on_gpu(torch.zeros((B, H, cap * (D + D // 16)), dtype=torch.uint8))
+    q = on_gpu(torch.zeros((rows, Hq, D))) if q is None else q
+    i32 = lambda n: on_gpu(torch.zeros((n,), dtype=torch.int32))  # noqa: E731
+    return cache, q, i32(B + 1), i32(B), 3, cap
+
+
+def part(buf, first, shape):
+    n = 1
+    for k in shape:
+        n *= k
+    return on_gpu(buf[first:first + n].view(shape))
+
+
+def test_attention_refuses_an_output_over_what_it_reads(calls):
+    buf = torch.zeros((3 * 5 * 4 * 64,))
+    q, n = part(buf, 0, (5, 4, 64)), 5 * 4 * 64
+    lv.cache4_attn(*attn_args(q=q), out=part(buf, n, (5, 4, 64)))
+    assert len(calls) == 1
+    for first in (0, 256, n - 4):
+        with pytest.raises(ValueError, match="out"):
+            lv.cache4_attn(*attn_args(q=q), out=part(buf, first, (5, 4, 64)))
+    with pytest.raises(ValueError, match="out"):
+        lv.cache4_attn(*attn_args(q=part(buf, 4, (5, 4, 64))), out=part(buf, 0, (5, 4, 64)))
+    # over the cache
+    a = attn_args(q=q)
+    with pytest.raises(ValueError, match="out"):
+        lv.cache4_attn(*a, out=on_gpu(a[0].view(-1)[64:64 + 4 * n].view(torch.float32).view(5, 4, 64)))
+    # over the weights
+    w = part(buf, n, (2, 2, 64))
+    for kw in (dict(weight=w), dict(weight_out=w)):
+        with pytest.raises(ValueError, match="out"):
+            lv.cache4_attn(*attn_args(q=q), out=part(buf, n + 128, (5, 4, 64)), weight_rows=1, **kw)
+    assert len(calls) == 1
