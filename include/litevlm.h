@@ -545,7 +545,9 @@ litevlm_status_t litevlm_cache4_append(int32_t dtype, int32_t B, int32_t Hkv, in
  * and v is the row at position start[b] + i of sample b, for
  * i < min(cu_rows[b+1] - cu_rows[b], max_rows); a position outside [0, cap) gives
  * zeros. Every finite cached value is exact in bf16 and fp32. Arguments as for
- * litevlm_cache4_append, with k and v the outputs (dtype F32 or BF16).
+ * litevlm_cache4_append, with k and v the outputs (dtype F32 or BF16), of cu_rows[B]
+ * rows at least; they overlap neither each other nor an input (of this the library,
+ * which does not know the rows, sees only k == v: LITEVLM_ERR_BAD_VALUE).
  */
 litevlm_status_t litevlm_cache4_read(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap,
                                      int32_t max_rows, const void* cache, const int32_t* start,

@@ -402,18 +402,25 @@ def cache4_append(cache: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_new:
 def cache4_read(cache: torch.Tensor, D: int, cu_rows: torch.Tensor, start: torch.Tensor, max_rows: int,
                 rows: Optional[int] = None, dtype: torch.dtype = torch.bfloat16, out: Optional[tuple] = None):
     """The values of cached rows: rows cu_rows[b].. of the packed result are positions start[b]..
-    of sample b. Returns (k, v) [rows,Hkv,D]; without `out` they have `rows` rows (B * max_rows by
-    default) of `dtype`, and rows past cu_rows[B] are not written."""
+    of sample b. Returns (k, v) [rows,Hkv,D]; without `out` they have `rows` rows of `dtype`, and rows
+    past cu_rows[B] are not written. `rows` is at least cu_rows[B]: the default, B * max_rows, is
+    where no sample asks for more than max_rows."""
     dev = cache.get_device()
     B, Hkv, cap, cptr = _cache_shape(cache, D, dev)
-    if out is None:
+    fresh = out is None
+    if fresh:
         shape = (B * max_rows if rows is None else rows, Hkv, D)
         out = (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
     k, v = out
     shape = (k.shape[0], Hkv, D)
+    kptr, vptr = _arg("k", k, k.dtype, shape, dev), _arg("v", v, k.dtype, shape, dev)
+    if shape[0] and not fresh:
+        n = k.nbytes
+        if _overlap(kptr, n, vptr, n) or _overlap(kptr, n, cptr, cache.nbytes) or _overlap(vptr, n, cptr, cache.nbytes):
+            raise ValueError("out: k, v and the cache overlap")
     _enqueue("litevlm_cache4_read", dev, _float_code("k", k), B, Hkv, D, cap, max_rows, cptr,
              _arg("start", start, torch.int32, (B,), dev), _arg("cu_rows", cu_rows, torch.int32, (B + 1,), dev),
-             _arg("k", k, k.dtype, shape, dev) or cptr, _arg("v", v, k.dtype, shape, dev) or cptr)
+             kptr or cptr, vptr or cptr + 16)
     return k, v
 
 

@@ -603,6 +603,7 @@ litevlm_status_t litevlm_cache4_read(int32_t dtype, int32_t B, int32_t Hkv, int3
                                      const int32_t* cu_rows, void* k, void* v, void* stream) {
   const litevlm_status_t st = check_cache4_rows(dtype, B, Hkv, D, cap, max_rows, k, v, cu_rows, start, cache);
   if (st != LITEVLM_OK) return st;
+  if (k == v && max_rows > 0) return LITEVLM_ERR_BAD_VALUE;
   Cache4RowsArgs a{};
   a.dtype = dtype;
   a.B = B;

@@ -156,3 +156,31 @@ def test_attention_refuses_an_output_over_what_it_reads(calls):
         with pytest.raises(ValueError, match="out"):
             lv.cache4_attn(*attn_args(q=q), out=part(buf, n + 128, (5, 4, 64)), weight_rows=1, **kw)
     assert len(calls) == 1
+
+
+def test_read_refuses_outputs_over_each_other_and_the_cache(calls):
+    cache, i32 = on_gpu(torch.zeros((2, 2, 64 * 136), dtype=torch.uint8)), lambda n: on_gpu(torch.zeros((n,), dtype=torch.int32))
+    buf = torch.zeros((2 * 5 * 2 * 128 + 4,))
+    n, shape = 5 * 2 * 128, (5, 2, 128)
+    read = lambda k, v: lv.cache4_read(cache, 128, i32(3), i32(2), 3, out=(k, v))  # noqa: E731
+    read(part(buf, 0, shape), part(buf, n, shape))
+    read(part(buf, n + 4, shape), part(buf, 4, shape))
+    assert len(calls) == 2
+    inside = on_gpu(cache.view(-1)[:4 * n].view(torch.float32).view(shape))
+    for k, v in ((part(buf, 0, shape), part(buf, 0, shape)), (part(buf, 0, shape), part(buf, n - 4, shape)),
+                 (part(buf, 4, shape), part(buf, 0, shape)), (inside, part(buf, 0, shape)), (part(buf, 0, shape), inside)):
+        with pytest.raises(ValueError, match="overlap"):
+            read(k, v)
+    assert len(calls) == 2
+    # without rows there is nothing to share
+    none = torch.zeros((0, 2, 128))
+    lv.cache4_read(cache, 128, i32(3), i32(2), 3, out=(on_gpu(none), on_gpu(none)))
+    k, v = calls[-1][2][-2:]
+    assert k != v and k % 16 == v % 16 == 0
+
+
+def test_read_refuses_one_address_for_keys_and_values():
+    read = lambda k, v, B=2: lv.load().litevlm_cache4_read(lv._abi.BF16, B, 2, 128, 64, 8, at(2), at(3), at(4), k, v,  # noqa: E731
+                                                           None)
+    assert read(at(0), at(0)) == lv._abi.ERR_BAD_VALUE
+    assert read(at(0), at(0), B=0) == lv._abi.ERR_BAD_SHAPE
