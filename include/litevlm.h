@@ -587,7 +587,7 @@ size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32
  *   q                  dev [total, Hq, D], total = cu_q[B]
  *   cu_q               dev int32 [B+1], non-decreasing, cu_q[0] = 0
  *   lengths            dev int32 [B]
- *   softmax_scale      finite, > 0
+ *   softmax_scale      > 0; it and its product with log2(e) finite in fp32
  *   o                  dev out [total, Hq, D]; rows past total are untouched
  *   weight_in          dev fp32 [B, Hkv, cap], or NULL = 0 (ignored when weight_rows is 0)
  *   weight_out         dev out fp32 [B, Hkv, cap], required when weight_rows > 0 (may be

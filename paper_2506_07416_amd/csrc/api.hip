@@ -637,7 +637,8 @@ litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32
   if (st != LITEVLM_OK) return st;
   if (max_len > cap) return LITEVLM_ERR_BAD_SHAPE;
   if (weight_rows > 0 && !weight_out) return LITEVLM_ERR_NULL_POINTER;
-  if (!finite_pos(softmax_scale) || o == q) return LITEVLM_ERR_BAD_VALUE;
+  const float scale_log2 = (float)((double)softmax_scale * 1.4426950408889634);
+  if (!finite_pos(softmax_scale) || !finite_pos(scale_log2) || o == q) return LITEVLM_ERR_BAD_VALUE;
   const void* big[] = {q, cache, o, workspace};
   for (const void* p : big)
     if (p && !aligned(p, 16)) return LITEVLM_ERR_MISALIGNED;
@@ -665,7 +666,7 @@ litevlm_status_t litevlm_cache4_attn(int32_t dtype, int32_t B, int32_t Hq, int32
   a.cu_q = cu_q;
   a.cache = cache;
   a.lengths = lengths;
-  a.scale_log2 = (float)((double)softmax_scale * 1.4426950408889634);
+  a.scale_log2 = scale_log2;
   a.o = o;
   a.weight_in = weight_in;
   a.weight_out = weight_out;

@@ -184,3 +184,11 @@ def test_read_refuses_one_address_for_keys_and_values():
                                                            None)
     assert read(at(0), at(0)) == lv._abi.ERR_BAD_VALUE
     assert read(at(0), at(0), B=0) == lv._abi.ERR_BAD_SHAPE
+
+
+def test_attention_refuses_scales_beyond_fp32():
+    """The kernels take logits to the base 2: softmax_scale * log2(e), which 2.4e38 carries past fp32."""
+    for scale in (2.4e38, 3.4e38):
+        assert attn(scale=scale) == lv._abi.ERR_BAD_VALUE
+    for scale in (2.3e38, 1e-45):
+        assert attn(scale=scale) == lv._abi.ERR_WORKSPACE
