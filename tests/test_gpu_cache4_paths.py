@@ -39,6 +39,9 @@ PATHS = [
     ([2700], [299], 4, 1, 64, 2720, "bf16", 1, 20),
     ([3100], [300], 4, 1, 128, 3104, "bf16", 300, 0),
     ([3100, 20], [130, 200], 4, 1, 128, 3104, "f32", 1, 0),
+    # few splits of two row tiles at D = 64
+    ([900, 899, 30, 512, 1, 0, 640, 700], [9, 8, 9, 1, 3, 9, 5, 2], 32, 16, 64, 928, "bf16", 4, 0),
+    ([900, 257, 30, 512, 1, 0, 640, 899], [9, 8, 9, 1, 3, 9, 5, 2], 32, 16, 64, 928, "f32", 9, 5),
     # up to 512 keys with 17..32 rows: one workgroup a head, weights added by it or not
     ([512, 300], [7, 8], 8, 2, 64, 512, "f32", 2, 0),
     ([511, 31], [8, 5], 8, 2, 64, 512, "bf16", 2, 1),
