@@ -18,7 +18,7 @@ def ceil(a, b):
 
 
 def form(dtype, B, Hq, H, D, max_q, max_len, weight_rows):
-    """(row tiles, splits, what becomes of the logits, workspace bytes)."""
+    """(row tiles, splits, what becomes of the logits, keys past the caches, workspace bytes)."""
     G = Hq // H
     rows, wrows, heads = max_q * G, weight_rows * G, B * H
     if rows <= 16:
@@ -40,12 +40,13 @@ def form(dtype, B, Hq, H, D, max_q, max_len, weight_rows):
     kept = weights and wrows <= 8
     whole = kept and splits == 1 and blocks == 1 and max_len <= 512
     logits = "lds" if whole else "kept" if kept else "again" if weights else "none"
+    once = blocks == 1 and max_len * (D + D // 16) * heads > 128 << 20
     up = lambda x: (x + 255) & ~255  # noqa: E731
     total = up(heads * rows * splits * D * 4 if splits > 1 else 0)
     total += up(heads * rows * splits * 8 if splits > 1 or logits == "kept" else 0)
     total += up(heads * wrows * 8 if weights and not whole else 0)
     total += up(heads * wrows * ceil(max_len, 32) * 128 if logits == "kept" else 0)
-    return tiles, splits, logits, max(total, 16)
+    return tiles, splits, logits, once, max(total, 16)
 
 
 def sizes():
@@ -54,6 +55,9 @@ def sizes():
         for lens, nq, Hq, H, D, cap, dtype, wr, extra in cases:
             for w in (wr, 0):
                 yield dtype, len(lens), Hq, H, D, max(nq), min(cap, max(lens) + extra), w
+    for (B, Hq, H, D, cap, mq), dtype in itertools.product(paths.LONG, DT):
+        for w in (0, 1, 3):
+            yield dtype, B, Hq, H, D, mq, cap, w
 
 
 def test_rule_is_the_library_s():
@@ -66,10 +70,11 @@ def test_every_form_has_a_case(dtype, D):
     hit = set()
     for s in sizes():
         if s[0] == dtype and s[4] == D:
-            tiles, splits, logits, _ = form(*s)
-            hit.add((tiles, logits))
+            tiles, splits, logits, once, _ = form(*s)
+            hit.add((tiles, logits, once))
             hit.add((tiles, "unsplit" if splits == 1 else "few" if splits <= 4 else "many"))
     for tiles in (1, 2):
-        want = {(tiles, x) for x in ("lds", "kept", "again", "none")}
+        want = {(tiles, x, False) for x in ("lds", "kept", "again", "none")}
+        want |= {(tiles, x, True) for x in ("kept", "again", "none")}
         want |= {(tiles, x) for x in ("unsplit", "few", "many")}
         assert want <= hit, sorted(want - hit, key=str)

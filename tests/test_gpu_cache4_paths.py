@@ -1,9 +1,11 @@
 """GPU parity of the attention over the 4-bit cache in every form that its sizes
 choose: one and two row tiles, keys unsplit, in few and in many splits, logits kept
-in LDS, kept in the workspace, taken again and not wanted. Bounds as in
-test_gpu_cache4. tests/test_cache4_paths.py checks on the host that the cases here
+in LDS, kept in the workspace, taken again and not wanted, keys of caches beyond
+128 MiB. Bounds as in test_gpu_cache4. tests/test_cache4_paths.py checks on the host that the cases here
 reach every form.
 """
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -99,6 +101,99 @@ def test_attention_forms_match_oracle(case):
     o3 = lv.cache4_attn(*args)
     check_attn(cache, q, cu, lens, Hq, D, dtype, 0, None, o3.double().cpu().numpy()[:cu[-1]], None,
                f"form {case}, no weights")
+
+
+# batch, Hq, H, D, cap, queries of a sample at most: caches just over 128 MiB, one block of rows
+LONG = [(16, 32, 8, 128, 7744, 3), (16, 32, 8, 128, 7744, 5), (32, 32, 8, 64, 7744, 3), (32, 32, 8, 64, 7744, 5)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_attention_of_caches_beyond_the_last_level_cache(case, dtype):
+    """Random codes and scales everywhere; three samples' first and last heads against the oracle."""
+    B, Hq, H, D, cap, mq = LONG[case]
+    assert B * H * cap * (D + D // 16) > 128 << 20
+    rng = np.random.default_rng(800 + case)
+    gen = torch.Generator(device="cuda").manual_seed(800 + case)
+    half = cap * D
+    cache = torch.randint(0, 256, (B, H, half + cap * D // 16), generator=gen, device="cuda", dtype=torch.uint8)
+    cache[:, :, half:] = cache[:, :, half:] % 5 + 122
+    lens = rng.integers(cap // 2, cap + 1, B)
+    lens[0], lens[B // 2] = cap, 37
+    nq = rng.integers(1, mq + 1, B)
+    nq[B - 1], nq[0] = mq, mq - 1
+    cu = cumulate(nq)
+    qt = torch.as_tensor(rng.standard_normal((cu[-1], Hq, D)) * 2).to(DT[dtype])
+    qd = qt.cuda()
+    G = Hq // H
+    for wr in (0, 1, 3):
+        log(f"long caches: batch {B} heads {Hq}/{H} D {D} {dtype}, up to {mq} queries, weight rows {wr}")
+        w0 = torch.rand((B, H, cap), generator=gen, device="cuda")
+        wo = w0.clone()
+        o = lv.cache4_attn(cache, qd, dev(cu), dev(lens), mq, cap, weight=w0, weight_out=wo, weight_rows=wr)
+        for b in (0, B // 2, B - 1):
+            heads = [0, H - 1]
+            rows = slice(cu[b], cu[b + 1])
+            qh = [g * G + i for g in heads for i in range(G)]
+            pick = lambda t: t[b:b + 1, heads].double().cpu().numpy()  # noqa: E731
+            check_attn(cache[b:b + 1, heads].cpu().numpy(), qt[rows][:, qh].double().numpy(), np.array([0, nq[b]]),
+                       [int(lens[b])], 2 * G, D, dtype, wr, pick(w0), o[rows][:, qh].double().cpu().numpy(), pick(wo),
+                       f"sample {b}")
+
+
+def test_attention_of_random_rows_beyond_32_bit_offsets():
+    """16777216 rows of two heads of random codes, in 64 bits on the GPU by parts.
+
+    The kernels add: in a wave, 16 steps of 32 keys in the matrix products (at most 512
+    roundings) or 8 exponentials a lane (128); 4 waves; 8192 splits by 8 slots of 1024,
+    then the slots. So an output is within 1600 roundings of fp32, 2^-24 of the sum of
+    p |V| each, and the sum of a softmax within 300; the logits as in check_attn."""
+    cap, D, H = lv._abi.MAX_CACHE4, 128, 2
+    log("16777216 random rows of two heads")
+    gen = torch.Generator(device="cuda").manual_seed(900)
+    cache = torch.empty((1, H, cap * (D + D // 16)), dtype=torch.uint8, device="cuda")
+    for g in range(H):  # by heads and parts: whole numbers of 8 bytes at a time
+        cache[0, g, :cap * D].random_(0, 256, generator=gen)
+        cache[0, g, cap * D:].random_(122, 127, generator=gen)
+    q = torch.randn((1, H, D), generator=gen, device="cuda")
+    w = torch.full((1, H, cap), 9.0, device="cuda")
+    n = cap - 5
+    o = lv.cache4_attn(cache, q, dev([0, 1]), dev([n]), 1, cap, weight_out=w, weight_rows=1)
+    assert (w[:, :, n:] == 9).all()
+    code = torch.tensor(list(c4.E2M1) + [-x for x in c4.E2M1], dtype=torch.float64, device="cuda")
+    part = 1 << 19
+    for g in range(H):
+        kc, vc = (cache[0, g, i * cap * D // 2:(i + 1) * cap * D // 2].view(cap, D // 2) for i in (0, 1))
+        ks, vs = (cache[0, g, cap * D + i * cap * 4:cap * D + (i + 1) * cap * 4].view(4, cap) for i in (0, 1))
+
+        def rows(codes, scales, j):
+            c = codes[j:j + part].long()
+            x = torch.stack((code[c & 15], code[c >> 4]), -1).view(-1, 4, 32)
+            s = torch.exp2(scales[:, j:j + part].double().T - 127)
+            return (x * s[:, :, None]).view(-1, D)
+
+        x = torch.empty((cap,), dtype=torch.float64, device="cuda")
+        size = 0.0
+        qg = q[0, g].double()
+        for j in range(0, cap, part):
+            k = rows(kc, ks, j)
+            x[j:j + part] = (k * qg).sum(-1) / math.sqrt(D)
+            size = max(size, float((k * qg).abs().sum(-1).max()) / math.sqrt(D))
+        x = x[:n]
+        p = torch.exp(x - x.max())
+        p /= p.sum()
+        want, A = (torch.zeros((D,), dtype=torch.float64, device="cuda") for _ in range(2))
+        for j in range(0, n, part):
+            v = rows(vc, vs, j)[:n - j]
+            pj = p[j:j + part, None]
+            want += (pj * v).sum(0)
+            A += (pj * v.abs()).sum(0)
+        rel = math.expm1(2 * size * (D + 4) * 2.0 ** -24) + 2.0 ** -22
+        err = (o[0, g].double() - want).abs()
+        assert (err <= (rel + 1900 * 2.0 ** -24) * A + 2.0 ** -23 * want.abs()).all(), float((err / A).max())
+        werr = ((w[0, g, :n].double() - p).abs() / p).max()
+        assert float(werr) <= rel + 310 * 2.0 ** -24, float(werr)
+        log(f"  head {g}: outputs {float((err / A).max()):.2e} of sum p|V|, weights {float(werr):.2e}")
 
 
 @pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
