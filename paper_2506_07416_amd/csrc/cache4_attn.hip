@@ -671,8 +671,12 @@ void launch_mt(const AttnParams& p, int B, const Cache4AttnLayout& lay, hipStrea
   const dim3 grid(p.Hkv * p.blocks * p.nsplit, B);
   // keys of more caches than the last-level cache holds half of, each read by one
   // workgroup, pass it by (493 MB of 32 samples: 119 -> 113 us with the join; at
-  // 3.7 MB, which stay in it, 4.6 -> 5.0 us)
-  const bool once = p.blocks == 1 && CacheHead<D>::bytes(p.max_len) * p.Hkv * B > ((int64_t)128 << 20);
+  // 3.7 MB, which stay in it, 4.6 -> 5.0 us), unless they are read again for the
+  // weights (4 queries, the whole call, past it and through it: 139 MB 82.2 and
+  // 80.1 us, 246 MB 136.8 and 134.2, 493 MB 261.7 and 264.2, there with 8 queries
+  // 282.7 and 281.5)
+  const bool once = (keep || p.wrows == 0) && p.blocks == 1 &&
+                    CacheHead<D>::bytes(p.max_len) * p.Hkv * B > ((int64_t)128 << 20);
   const auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, p); };
   if (lay.whole) {
     run(cache4_attn_kernel<D, TERMS, MT, kLds, false>);

@@ -40,7 +40,7 @@ def form(dtype, B, Hq, H, D, max_q, max_len, weight_rows):
     kept = weights and wrows <= 8
     whole = kept and splits == 1 and blocks == 1 and max_len <= 512
     logits = "lds" if whole else "kept" if kept else "again" if weights else "none"
-    once = blocks == 1 and max_len * (D + D // 16) * heads > 128 << 20
+    once = logits != "again" and blocks == 1 and max_len * (D + D // 16) * heads > 128 << 20
     up = lambda x: (x + 255) & ~255  # noqa: E731
     total = up(heads * rows * splits * D * 4 if splits > 1 else 0)
     total += up(heads * rows * splits * 8 if splits > 1 or logits == "kept" else 0)
@@ -75,6 +75,6 @@ def test_every_form_has_a_case(dtype, D):
             hit.add((tiles, "unsplit" if splits == 1 else "few" if splits <= 4 else "many"))
     for tiles in (1, 2):
         want = {(tiles, x, False) for x in ("lds", "kept", "again", "none")}
-        want |= {(tiles, x, True) for x in ("kept", "again", "none")}
+        want |= {(tiles, x, True) for x in ("kept", "none")}
         want |= {(tiles, x) for x in ("unsplit", "few", "many")}
         assert want <= hit, sorted(want - hit, key=str)
