@@ -387,9 +387,12 @@ __global__ __launch_bounds__(kOneThreads) void verify_one_kernel(VerifyParams p)
 
 template <bool BF16>
 void launch(const VerifyParams& p, int B, bool one, hipStream_t stream) {
-  // One launch while a workgroup keeps up: 2.3 us less for the host that launches and
-  // 2.4 for a workspace that is not needed (13.2 -> 8.9 us a pass), on the GPU alone, in a graph, 5.3, 6.2, 7.0 and 8.1 us for 1
-  // to 4 tiles against 6.4 for two launches.
+  // One launch up to the 64 parts that one wave scans, 32768 entries. The time of a
+  // program that launches call by call decides: 9.3-9.8 us a call for 8000 to 32000
+  // entries, 13.8-14.2 with two launches and the workspace that they need, at batches
+  // of 1, 16 and 64 alike. In a graph the two are within 1.5 us: 8000 entries 5.6-6.1
+  // and 6.7-7.4 us, 16000 6.4-7.0 and 6.7-8.0, 24000 7.4-8.7 and 6.8-8.8, 32000
+  // 8.3-9.8 and 6.9-9.5 (batch 1-64).
   if (one) {
     hipLaunchKernelGGL(verify_one_kernel<BF16>, dim3(B), dim3(kOneThreads), 0, stream, p);
   } else {
