@@ -573,9 +573,12 @@ size_t litevlm_cache4_attn_workspace(int32_t dtype, int32_t B, int32_t Hq, int32
  *   weight_out[b,g,j] = weight_in[b,g,j] + sum_{i < min(weight_rows, m_b)} sum_{h in g} p_i,h(j)
  * A query that sees no row (m_b > n_b) gives o = 0 and adds no weight. Softmax and
  * accumulation in fp32. For bf16 queries the probabilities are rounded to bf16
- * in front of the product with V (the weights and the softmax sum are not); for
- * fp32 queries (of 2^-100 and more) every product is exact in fp32. A probability below 2^-126 of its
- * row's largest counts as 0.
+ * in front of the product with V (the weights and the softmax sum are not); the same
+ * queries passed in fp32 keep them whole. For fp32 queries (of 2^-100 and more) every
+ * product is exact in fp32. A probability below 2^-126 of its row's largest counts as 0.
+ * Values: n_b * max|V| up to 2^119, beyond which a sum may pass fp32 where its quotient
+ * does not. Logits: a q . K, or its product with softmax_scale * log2(e), beyond fp32 is
+ * infinite: -inf has no weight; +inf, or nothing but -inf, makes the query's results NaN.
  *
  *   dtype              LITEVLM_F32 or LITEVLM_BF16 (q and o)
  *   B, Hq, Hkv, D      batch, heads (Hq % Hkv == 0), head dim (64 or 128)

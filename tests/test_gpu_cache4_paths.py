@@ -1,8 +1,8 @@
 """GPU parity of the attention over the 4-bit cache in every form that its sizes
 choose: one and two row tiles, keys unsplit, in few and in many splits, logits kept
 in LDS, kept in the workspace, taken again and not wanted, keys of caches beyond
-128 MiB. Bounds as in test_gpu_cache4. tests/test_cache4_paths.py checks on the host that the cases here
-reach every form.
+128 MiB; and numbers at the ends of the format. Bounds as in test_gpu_cache4.
+tests/test_cache4_paths.py checks on the host that the cases here reach every form.
 """
 import math
 
@@ -234,3 +234,72 @@ def test_nan_and_stale_rows_with_two_row_tiles_and_split_keys(dtype, D):
     assert torch.isfinite(w[0, 0]).all()
     # the query's probabilities are NaN for the rows that it sees, and for no other
     assert torch.isnan(w[0, 1, :at + 1]).all() and not w[0, 1, at + 1:].any()
+
+
+# ----------------------------------------------------------------------------- numbers at the format's ends
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_of_the_smallest_numbers(dtype):
+    """Blocks below 2^-126 keep the scale 2^-125, whose first step is 2^-126: what lies
+    above 2^-127 rounds up to it, a subnormal input or not."""
+    log(f"append of the smallest numbers, {dtype}")
+    D, cap = 64, 32
+    x = np.zeros((3, 1, D))
+    x[0, 0, :8] = np.array([1.0, 1.5, 1.01, 1.99, -1.5, -1.0, 0.99, 2.0]) * 2.0 ** -127
+    x[0, 0, 32:36] = np.array([3.0, 1.5, -2.5, 0.5]) * 2.0 ** -127     # beside a normal number
+    x[1, 0, :4] = np.array([12.0, 1.5, 7.0, -1.75]) * 2.0 ** -127
+    x[1, 0, 32:35] = [1.0, 1e-38, -1e-38]                           # far below the block's scale
+    x[2, 0, :] = 2.0 ** -127 * (1 + np.arange(D) / D)
+    kt = torch.as_tensor(x).float().to(DT[dtype])
+    cache = lv.cache4_empty(1, 1, D, cap)
+    lv.cache4_append(cache, kt.cuda(), kt.flip(0).cuda(), dev([0, 3]), dev([0]), 3)
+    got = c4.split_cache(cache.cpu().numpy(), D)
+    for t, codes, scales in ((kt, got[0], got[1]), (kt.flip(0), got[2], got[3])):
+        wc, ws = c4.encode(t.double().numpy()[:, 0])
+        assert np.array_equal(scales[0, 0, :3], ws) and np.array_equal(codes[0, 0, :3], wc)
+
+
+def test_read_of_every_scale():
+    """All 256 scale bytes with every code whose value fp32 has (bf16 then has it too),
+    the subnormal ones among them; byte 255 is NaN."""
+    log("every scale byte")
+    D, cap = 64, 256
+    codes = np.zeros((1, 1, cap, D), np.uint8)
+    codes[0, 0] = np.arange(D) % 16
+    codes[0, 0, 253] = [0, 1, 2, 3, 4, 5, 8, 9, 10, 11, 12, 13, 0, 1, 2, 3] * 4      # up to 3 * 2^126
+    codes[0, 0, 254] = [0, 1, 2, 3, 8, 9, 10, 11] * 8                                # up to 1.5 * 2^127
+    scales = np.broadcast_to(np.arange(256, dtype=np.uint8)[None, None, :, None], (1, 1, cap, 2))
+    cache = torch.as_tensor(c4.join_cache(codes, scales, codes[:, :, :, ::-1], scales)).cuda()
+    want = c4.decode(codes, scales)[0, 0]
+    for dt in (torch.bfloat16, torch.float32):
+        k, v = lv.cache4_read(cache, D, dev([0, cap]), dev([0]), cap, dtype=dt)
+        np.testing.assert_array_equal(k[:, 0].double().cpu().numpy(), want)
+        np.testing.assert_array_equal(v[:, 0].double().cpu().numpy(), want[:, ::-1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,m,top", [(512, 1, 107), (1500, 40, 105)])
+def test_attention_at_the_end_of_the_values_range(dtype, n, m, top):
+    """n rows of up to 6 * 2^top, n * max|V| just below 2^119: the largest that the header
+    allows. All keys but a wave's first have logits 7.9 (log2) above those: the reference
+    stays behind the maximum, where the unnormalised outputs are largest."""
+    log(f"values of up to 6 * 2^{top}, {n} rows, {m} queries, {dtype}")
+    assert 2.0 ** 118 < n * 6 * 2.0 ** top < 2.0 ** 119
+    rng = np.random.default_rng(970)
+    Hq, H, D, cap = 4, 1, 128, (n + 31) // 32 * 32
+    kc, ks, vc, vs = c4.split_cache(random_cache(rng, 1, H, D, cap), D)
+    kc[:], ks[:], vs[:] = 0, 127, top + 127
+    vc[..., :64] = 7                                   # half of the elements 6 * 2^top in every row: sums that grow
+    kc[0, 0, 128:, 0] = 2                              # 1.0, behind the four waves' first steps
+    cache = c4.join_cache(kc, ks, vc, vs)
+    qt = torch.zeros((m, Hq, D))
+    qt[..., 0] = 7.875 * math.log(2.0)
+    qt = qt.to(DT[dtype])
+    o = lv.cache4_attn(torch.as_tensor(cache).cuda(), qt.cuda(), dev([0, m]), dev([n]), m, n, softmax_scale=1.0)
+    K, V = c4.decode(kc, ks), c4.decode(vc, vs)
+    ref, _, A, size = c4.attention(qt.double().numpy(), [0, m], K, V, [n], 1.0)
+    got = o.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    rel = np.expm1(2 * size * (D + 4) * 2.0 ** -24)[..., None] + 2.0 ** -22
+    u = 2.0 ** -8 if dtype == "bf16" else 0.0
+    assert (np.abs(got - ref) <= (u + rel + (n + 8) * 2.0 ** -24) * A + (u + 2.0 ** -23) * np.abs(ref)).all()
