@@ -1,7 +1,8 @@
 """GPU parity of the attention over the 4-bit cache in every form that its sizes
 choose: one and two row tiles, keys unsplit, in few and in many splits, logits kept
 in LDS, kept in the workspace, taken again and not wanted, keys of caches beyond
-128 MiB; and numbers at the ends of the format. Bounds as in test_gpu_cache4.
+128 MiB; numbers at the ends of the format; and the cache behind the framework's own
+selection. Bounds as in test_gpu_cache4.
 tests/test_cache4_paths.py checks on the host that the cases here reach every form.
 """
 import math
@@ -11,8 +12,9 @@ import pytest
 import torch
 
 import paper_2506_07416_amd as lv
+import synth
 from oracle import cache4 as c4
-from parity_util import log
+from parity_util import log, to_device
 from test_gpu_cache4 import DT, check_attn, cumulate, dev, random_cache
 
 pytestmark = pytest.mark.gpu
@@ -303,3 +305,38 @@ def test_attention_at_the_end_of_the_values_range(dtype, n, m, top):
     rel = np.expm1(2 * size * (D + 4) * 2.0 ** -24)[..., None] + 2.0 ** -22
     u = 2.0 ** -8 if dtype == "bf16" else 0.0
     assert (np.abs(got - ref) <= (u + rel + (n + 8) * 2.0 ** -24) * A + (u + 2.0 ** -23) * np.abs(ref)).all()
+
+
+# ----------------------------------------------------------------------------- behind the framework's selection
+
+def test_selected_rows_enter_the_cache_and_are_attended_like_a_decode():
+    """The kept rows of the selection as they are packed, appended with their cu_seqlens;
+    the next token behind them; its attention against the decode attention over the same
+    rows read back. Both are within their own bounds of the 64-bit result."""
+    case = synth.config_case(4, Tv=64, T=16, keep_ratio=0.5)
+    q, k, v = (to_device(x, case.dtype) for x in (case.q, case.k, case.v))
+    logit = torch.from_numpy(case.view_logit).cuda()
+    _, keep, _ = lv.patch_select(logit, case.view_offsets, case.S, case.w_lexical, case.threshold)
+    r = lv.token_score_topk(q, k, v, keep, case.keep_ratio, case.V_full)
+    B, S, Hq, H, D = case.B, case.S, case.Hq, case.Hkv, case.D
+    cu = r["cu_seqlens"]
+    lens = (cu[1:] - cu[:-1]).cpu().numpy()
+    log(f"selected rows {lens.tolist()} into the 4-bit cache")
+    cap = (S + 1 + 31) // 32 * 32
+    cache = lv.cache4_empty(B, H, D, cap)
+    lv.cache4_append(cache, r["kc"], r["vc"], cu, dev([0] * B), S)
+    rng = np.random.default_rng(960)
+    q1, k1, v1 = (torch.as_tensor(rng.standard_normal((B, h, D))).to(torch.bfloat16).cuda() for h in (Hq, H, H))
+    one = dev(np.arange(B + 1))
+    lv.cache4_append(cache, k1, v1, one, dev(lens), 1)
+    o = lv.cache4_attn(cache, q1, one, dev(lens + 1), 1, S + 1)
+    check_attn(cache.cpu().numpy(), q1.double().cpu().numpy(), np.arange(B + 1), (lens + 1).tolist(), Hq, D, "bf16", 0, None,
+               o.double().cpu().numpy(), None, "the next token")
+    kr, vr = lv.cache4_read(cache, D, cu, dev([0] * B), S, rows=r["kc"].shape[0])
+    k1r, v1r = lv.cache4_read(cache, D, one, dev(lens), 1)
+    d = lv.decode_attn(q1, k1r, v1r, kr, vr, cu, S)
+    kc, ks, vc, vs = c4.split_cache(cache.cpu().numpy(), D)
+    _, _, A, _ = c4.attention(q1.double().cpu().numpy(), np.arange(B + 1), c4.decode(kc, ks), c4.decode(vc, vs), lens + 1,
+                              1 / math.sqrt(D))
+    # each call rounds its probabilities and its result to bf16: 2 * 2^-8 of sum p |V| a call
+    assert (np.abs((o.double() - d.double()).cpu().numpy()) <= 4.1 * 2.0 ** -8 * A).all()
