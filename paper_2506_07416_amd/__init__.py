@@ -358,11 +358,6 @@ def _workspace(t: Optional[torch.Tensor], dev: int) -> tuple:
     return t.data_ptr(), t.nbytes
 
 
-def _overlap(a: int, na: int, b: int, nb: int) -> bool:
-    """Whether na bytes at a and nb bytes at b, both some, share any."""
-    return a < b + nb and b < a + na
-
-
 def _cache_shape(cache: torch.Tensor, D: int, dev: int):
     """(B, Hkv, cap) of a cache tensor of head dim D on device `dev`, and its address."""
     if D not in (64, 128):
@@ -415,8 +410,8 @@ def cache4_read(cache: torch.Tensor, D: int, cu_rows: torch.Tensor, start: torch
     shape = (k.shape[0], Hkv, D)
     kptr, vptr = _arg("k", k, k.dtype, shape, dev), _arg("v", v, k.dtype, shape, dev)
     if shape[0] and not fresh:
-        n = k.nbytes
-        if _overlap(kptr, n, vptr, n) or _overlap(kptr, n, cptr, cache.nbytes) or _overlap(vptr, n, cptr, cache.nbytes):
+        n, end = k.nbytes, cptr + B * Hkv * cap * (D + D // 16)
+        if abs(kptr - vptr) < n or cptr < kptr + n and kptr < end or cptr < vptr + n and vptr < end:
             raise ValueError("out: k, v and the cache overlap")
     _enqueue("litevlm_cache4_read", dev, _float_code("k", k), B, Hkv, D, cap, max_rows, cptr,
              _arg("start", start, torch.int32, (B,), dev), _arg("cu_rows", cu_rows, torch.int32, (B + 1,), dev),
@@ -460,8 +455,10 @@ def cache4_attn(cache: torch.Tensor, q: torch.Tensor, cu_q: torch.Tensor, length
             wout = _arg("weight_out", weight_out, torch.float32, (B, Hkv, cap), dev)
     if rows and not fresh:
         n, nw = rows * Hq * D * (4 if code == _abi.F32 else 2), B * Hkv * cap * 4
-        if (_overlap(optr, n, qptr, n) or _overlap(optr, n, cptr, cache.nbytes)
-                or wout is not None and (_overlap(optr, n, wout, nw) or win is not None and _overlap(optr, n, win, nw))):
+        end = optr + n
+        if (qptr < end and optr < qptr + n or cptr < end and optr < cptr + B * Hkv * cap * (D + D // 16)
+                or wout is not None and (wout < end and optr < wout + nw
+                                         or win is not None and win < end and optr < win + nw)):
             raise ValueError("out: overlaps q, the cache or a weight")
     if workspace is None:
         n = load().litevlm_cache4_attn_workspace(code, B, Hq, Hkv, D, max_q, max_len, weight_rows)
