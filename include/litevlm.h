@@ -535,6 +535,8 @@ size_t litevlm_cache4_bytes(int32_t B, int32_t Hkv, int32_t D, int32_t cap);
  *   cache              dev, the 4-bit cache (in place)
  *   weight             dev fp32 [B, Hkv, cap] or NULL: set to 0 at the new positions
  *                      (the accumulated attention weights of litevlm_cache4_attn)
+ * Neither cache nor weight may overlap an input or the other (LITEVLM_ERR_BAD_VALUE; of
+ * k and v, whose rows only the device knows, the library sees nothing).
  */
 litevlm_status_t litevlm_cache4_append(int32_t dtype, int32_t B, int32_t Hkv, int32_t D, int32_t cap,
                                        int32_t max_new, const void* k, const void* v, const int32_t* cu_new,

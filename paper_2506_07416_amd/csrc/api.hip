@@ -582,6 +582,9 @@ litevlm_status_t litevlm_cache4_append(int32_t dtype, int32_t B, int32_t Hkv, in
   const litevlm_status_t st = check_cache4_rows(dtype, B, Hkv, D, cap, max_new, k, v, cu_new, start, cache);
   if (st != LITEVLM_OK) return st;
   if (weight && !aligned(weight, 4)) return LITEVLM_ERR_MISALIGNED;
+  const Span in[] = {{cu_new, (size_t)(B + 1) * 4}, {start, (size_t)B * 4}};
+  const Span out[] = {{cache, litevlm_cache4_bytes(B, Hkv, D, cap)}, {weight, (size_t)B * Hkv * cap * 4}};
+  if (overlap(in, out)) return LITEVLM_ERR_BAD_VALUE;
   Cache4RowsArgs a{};
   a.dtype = dtype;
   a.B = B;

@@ -192,3 +192,17 @@ def test_attention_refuses_scales_beyond_fp32():
         assert attn(scale=scale) == lv._abi.ERR_BAD_VALUE
     for scale in (2.3e38, 1e-45):
         assert attn(scale=scale) == lv._abi.ERR_WORKSPACE
+
+
+def test_append_refuses_weights_over_the_cache_and_either_over_its_counts():
+    bad, nbytes = lv._abi.ERR_BAD_VALUE, 2 * 2 * 64 * 136
+
+    def append(cu=at(2), start=at(3), cache=at(4), weight=at(5), B=2):
+        # with refused arguments only: an accepted call would be enqueued
+        return lv.load().litevlm_cache4_append(lv._abi.BF16, B, 2, 128, 64, 8, at(0), at(1), cu, start, cache, weight, None)
+
+    assert append(B=0) == lv._abi.ERR_BAD_SHAPE
+    for off in (0, nbytes - 4, 4 - 2 * 2 * 64 * 4):
+        assert append(weight=at(4) + off) == bad, off
+    assert append(weight=at(2)) == bad and append(weight=at(3) + 4) == bad
+    assert append(cache=at(2) & ~15) == bad and append(start=at(4) + 32) == bad
